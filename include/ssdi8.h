@@ -50,7 +50,9 @@ typedef enum {
   SSDI8_ERR_ARG = 7           /* an enum / flag / shift argument is out of range             */
 } ssdi8_status;
 
-typedef enum { SSDI8_F32 = 0, SSDI8_F16 = 1 } ssdi8_dtype;
+/* SSDI8_BF16, SSDI8_I8: of the operators around the layer (below); the layer's own calls take fp16
+   and fp32. */
+typedef enum { SSDI8_F32 = 0, SSDI8_F16 = 1, SSDI8_BF16 = 2, SSDI8_I8 = 3 } ssdi8_dtype;
 
 /* Quantization granules of a logical [b, l, k, m] tensor. */
 typedef enum {
@@ -333,6 +335,150 @@ typedef struct {
 } ssdi8_calib_args;
 size_t ssdi8_calibrate_workspace_size(const ssdi8_dims* d);
 ssdi8_status ssdi8_calibrate(const ssdi8_dims* d, const ssdi8_calib_args* a, void* stream);
+
+/*
+ * Operators around the SSD layer in a block: the short causal convolution in front of it, a
+ * selective scan for any length and for a decay per channel and state, the gated norm behind it and
+ * the projections.  What they share, beside the conventions above:
+ *   - Types: fp32, fp16 or bf16 activations (the projections: fp16, bf16 or int8); parameters,
+ *     states of the scan and every sum in fp32 (int8 products in int32).
+ *   - Layouts: the last dimension is dense; batch elements and tokens (rows) lie at strides given in
+ *     elements, 0 or more, so that a slice of a projection's output is read where it lies.
+ *     Outputs and states are dense unless a stride is given.  Pointers need the alignment of their
+ *     element only (a scan's state for one token: 16 bytes).
+ *   - `lengths`: NULL, or device int32 [batch]: tokens of batch element b at or behind lengths[b]
+ *     (taken into [0, seqlen]) are not read, give y = 0 and leave the state as it is.
+ *   - An output may not overlap an input, except where a call says so.
+ *   - batch = 0 or no rows: nothing is done.  seqlen = 0: the final state is the initial one.
+ */
+
+/*
+ * ssdi8_causal_conv — causal convolution of every channel over its last `width` tokens:
+ *     y[b,t,d] = act(bias[d] + sum_{j < width} weight[d,j] x[b, t-(width-1)+j, d])
+ * where x before token 0 is init_state[b, :, d], the width - 1 inputs before it (NULL: zeros).  The
+ * columns of y go to up to three dense tensors: y[0] takes the first y_cols[0], and so on (unused:
+ * y NULL, y_cols 0; their sum is `channels`), e.g. x, B and C of the SSD layer.
+ * final_state (NULL: not wanted) receives the last width - 1 inputs and may be init_state.
+ */
+typedef enum {
+  SSDI8_ACT_NONE = 0,
+  SSDI8_ACT_SILU = 1,       /* v / (1 + exp(-v))                                      */
+  SSDI8_ACT_GELU = 2,       /* v (1 + erf(v / sqrt(2))) / 2          (projections)    */
+  SSDI8_ACT_SOFTPLUS = 3    /* log(1 + exp(v)), v above 20           (projections)    */
+} ssdi8_act;
+
+typedef struct {
+  int dtype;                          /* of x, states and y                                       */
+  const void* x;                      /* [batch, seqlen, channels]                                */
+  int64_t x_batch_stride, x_token_stride;
+  const float* weight; int width;     /* [channels, width], width 2, 3 or 4                       */
+  const float* bias;                  /* [channels] or NULL                                       */
+  int act;                            /* SSDI8_ACT_NONE or SSDI8_ACT_SILU                         */
+  const void* init_state;             /* [batch, width-1, channels] or NULL                       */
+  const int* lengths;                 /* [batch] or NULL                                          */
+  void* y[3]; int64_t y_cols[3];      /* [batch, seqlen, y_cols[i]]                               */
+  void* final_state;                  /* [batch, width-1, channels] or NULL                       */
+} ssdi8_conv_args;
+ssdi8_status ssdi8_causal_conv(int64_t batch, int64_t seqlen, int64_t channels,
+                               const ssdi8_conv_args* a, void* stream);
+
+/* ssdi8_causal_conv_step — one token of every sequence: x [batch, channels] at x_batch_stride, y[i]
+   [batch, y_cols[i]]; final_state, in and out, holds the inputs before the token and then the last
+   ones including it.  init_state, lengths and x_token_stride are not used. */
+ssdi8_status ssdi8_causal_conv_step(int64_t batch, int64_t channels, const ssdi8_conv_args* a,
+                                    void* stream);
+
+/*
+ * ssdi8_selective_scan — the unquantized recurrence itself, token by token.  Channel d of D = nheads *
+ * headdim belongs to head h = d / headdim and reads group d / (D / ngroups) of B and C:
+ *     delta  = dt[b,t,h] + dt_bias[h], after softplus when dt_softplus
+ *     s[d,n] = exp(delta A) s[d,n] + delta u[b,t,d] B[b,t,g,n]       A = A[d,n], or A[h] when tied
+ *     y      = sum_n C[b,t,g,n] s[d,n] + D[h] u, times silu(z[b,t,d]) when z is given
+ * headdim 1 with A [D,N] is the form with a time step and decays per channel; tied with headdim 64
+ * and N = 128 is the SSD layer's recurrence, for lengths that are no multiple of its chunk (its fp32
+ * final states are this call's initial states and the other way round).  Any seqlen; dstate up to
+ * 256; D a multiple of ngroups.  init_state and final_state may be the same memory.
+ */
+typedef struct {
+  int dtype;                          /* of u, B, C, z and y                                      */
+  int dt_dtype;                       /* of dt: SSDI8_F32 or the same                             */
+  const void* u;                      /* [batch, seqlen, D]                                       */
+  int64_t u_batch_stride, u_token_stride;
+  const void* dt;                     /* [batch, seqlen, nheads]                                  */
+  int64_t dt_batch_stride, dt_token_stride;
+  int dt_softplus;
+  const float* dt_bias;               /* [nheads] or NULL                                         */
+  const float* A; int tied;           /* [D, dstate], or [nheads] when tied (<= 0)                */
+  const void* B;                      /* [batch, seqlen, ngroups, dstate]                         */
+  int64_t B_batch_stride, B_token_stride;
+  const void* C;                      /* as B                                                     */
+  int64_t C_batch_stride, C_token_stride;
+  const float* D;                     /* [nheads] or NULL (= 0)                                   */
+  const void* z;                      /* [batch, seqlen, D] or NULL                               */
+  int64_t z_batch_stride, z_token_stride;
+  const float* init_state;            /* [batch, D, dstate] or NULL (= 0)                         */
+  const int* lengths;                 /* [batch] or NULL                                          */
+  void* y;                            /* [batch, seqlen, D]                                       */
+  float* final_state;                 /* [batch, D, dstate] or NULL                               */
+  void* workspace; size_t workspace_bytes;
+} ssdi8_sel_scan_args;
+typedef struct {
+  int64_t batch, seqlen, nheads, headdim, ngroups, dstate;
+} ssdi8_sel_scan_dims;
+/* 0 where none is needed (the workspace may then be NULL), and on invalid sizes. */
+size_t ssdi8_selective_scan_workspace_size(const ssdi8_sel_scan_dims* d);
+ssdi8_status ssdi8_selective_scan(const ssdi8_sel_scan_dims* d, const ssdi8_sel_scan_args* a,
+                                  void* stream);
+
+/* ssdi8_selective_scan_step — one token of every sequence (d->seqlen is not used): u, z, y [batch, D],
+   dt [batch, nheads], B, C [batch, ngroups, dstate] at their batch strides; final_state, in and out, is
+   the state before and after the token (16-byte aligned).  No workspace; init_state, lengths and
+   token strides are not used. */
+ssdi8_status ssdi8_selective_scan_step(const ssdi8_sel_scan_dims* d, const ssdi8_sel_scan_args* a,
+                                       void* stream);
+
+/*
+ * ssdi8_gated_norm — RMS norm of rows in `groups` equal groups of channels, with an optional residual
+ * in front and an optional gate:
+ *     s = x + residual (residual_out = s, rounded; it may be the residual itself)
+ *     y = v rsqrt(mean_group(v^2) + eps) weight,  v = s silu(z)      (norm_before_gate = 0)
+ *     y = s rsqrt(mean_group(s^2) + eps) weight silu(z)              (norm_before_gate = 1)
+ * x and z at row strides, the others dense; y may be x where x is dense.  At most 32768 channels per
+ * group; eps >= 0, finite.
+ */
+typedef struct {
+  int dtype;
+  const void* x; int64_t x_row_stride;      /* [rows, channels]                                   */
+  const void* z; int64_t z_row_stride;      /* [rows, channels] or NULL                           */
+  const void* residual;                     /* [rows, channels] or NULL                           */
+  const float* weight;                      /* [channels]                                         */
+  float eps; int norm_before_gate;
+  void* y;                                  /* [rows, channels]                                   */
+  void* residual_out;                       /* [rows, channels], with a residual                  */
+} ssdi8_norm_args;
+ssdi8_status ssdi8_gated_norm(int64_t rows, int64_t channels, int64_t groups,
+                              const ssdi8_norm_args* a, void* stream);
+
+/*
+ * ssdi8_linear — a projection with its epilogue:
+ *     y[r,o] = act(s sum_k x[r,k] weight[o,k] + bias[o]) + residual[r,o]
+ * with s = 1 (fp16, bf16: products in fp32) or x_scale[r] weight_scale[o] (int8: products in int32; the
+ * codes and per-token steps of ssdi8_quantize_act with SSDI8_GRAN_TOKEN, and weights quantized per
+ * output).  y and the residual are fp32 or x's type (int8: fp16).  k >= 1, up to 131072 for int8.
+ */
+typedef struct {
+  int dtype;                                /* of x and weight: SSDI8_F16, SSDI8_BF16, SSDI8_I8   */
+  const void* x; int64_t x_row_stride;      /* [rows, k]                                          */
+  const void* weight; int64_t weight_row_stride;   /* [outputs, k]                                */
+  const float* x_scale;                     /* [rows] (int8 only)                                 */
+  const float* weight_scale;                /* [outputs] (int8 only)                              */
+  const float* bias;                        /* [outputs] or NULL                                  */
+  int act;                                  /* ssdi8_act                                          */
+  const void* residual; int64_t residual_row_stride;   /* [rows, outputs] or NULL                 */
+  void* y; int64_t y_row_stride; int y_dtype;          /* [rows, outputs]; may be the residual    */
+} ssdi8_linear_args;
+ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_linear_args* a,
+                          void* stream);
 
 /*
  * ssdi8_mfma_probe — measurement helper: the on-box peak rate of the matrix cores, the

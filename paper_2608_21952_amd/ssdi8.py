@@ -11,6 +11,7 @@ the errors.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Dict, Iterable, Optional, Tuple
@@ -21,7 +22,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libssdi8.so")
 
 OK, ERR_NULL, ERR_SHAPE, ERR_UNSUPPORTED, ERR_ALIGN, ERR_WORKSPACE, ERR_HIP, ERR_ARG = range(8)
-F32, F16 = 0, 1
+F32, F16, BF16, I8 = 0, 1, 2, 3
+ACT = {None: 0, "none": 0, "silu": 1, "gelu": 2, "softplus": 3}
 GRAN = {"tensor": 0, "group": 1, "channel": 2, "token": 3}
 P_DIM, N_DIM, CHUNK = 64, 128, 256
 
@@ -89,6 +91,49 @@ class CalibArgs(ctypes.Structure):
     ]
 
 
+_L = ctypes.c_int64
+
+
+class ConvArgs(ctypes.Structure):
+    _fields_ = [
+        ("dtype", _I), ("x", _P), ("x_batch_stride", _L), ("x_token_stride", _L), ("weight", _P),
+        ("width", _I), ("bias", _P), ("act", _I), ("init_state", _P), ("lengths", _P),
+        ("y", _P * 3), ("y_cols", _L * 3), ("final_state", _P),
+    ]
+
+
+class SelScanDims(ctypes.Structure):
+    _fields_ = [(n, _L) for n in ("batch", "seqlen", "nheads", "headdim", "ngroups", "dstate")]
+
+
+class SelScanArgs(ctypes.Structure):
+    _fields_ = [
+        ("dtype", _I), ("dt_dtype", _I), ("u", _P), ("u_batch_stride", _L), ("u_token_stride", _L),
+        ("dt", _P), ("dt_batch_stride", _L), ("dt_token_stride", _L), ("dt_softplus", _I),
+        ("dt_bias", _P), ("A", _P), ("tied", _I), ("B", _P), ("B_batch_stride", _L),
+        ("B_token_stride", _L), ("C", _P), ("C_batch_stride", _L), ("C_token_stride", _L), ("D", _P),
+        ("z", _P), ("z_batch_stride", _L), ("z_token_stride", _L), ("init_state", _P),
+        ("lengths", _P), ("y", _P), ("final_state", _P), ("workspace", _P),
+        ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class NormArgs(ctypes.Structure):
+    _fields_ = [
+        ("dtype", _I), ("x", _P), ("x_row_stride", _L), ("z", _P), ("z_row_stride", _L),
+        ("residual", _P), ("weight", _P), ("eps", ctypes.c_float), ("norm_before_gate", _I),
+        ("y", _P), ("residual_out", _P),
+    ]
+
+
+class LinearArgs(ctypes.Structure):
+    _fields_ = [
+        ("dtype", _I), ("x", _P), ("x_row_stride", _L), ("weight", _P), ("weight_row_stride", _L),
+        ("x_scale", _P), ("weight_scale", _P), ("bias", _P), ("act", _I), ("residual", _P),
+        ("residual_row_stride", _L), ("y", _P), ("y_row_stride", _L), ("y_dtype", _I),
+    ]
+
+
 _lib = None
 _native = None    # the native marshalling, loaded with the library
 
@@ -130,6 +175,21 @@ def lib() -> ctypes.CDLL:
     L.ssdi8_mfma_probe.argtypes = [_I, ctypes.c_int64, ctypes.c_int64, _P,
                                    ctypes.POINTER(ctypes.c_int64), _P]
     L.ssdi8_mfma_probe.restype = _I
+    L.ssdi8_causal_conv.argtypes = [i64, i64, i64, ctypes.POINTER(ConvArgs), _P]
+    L.ssdi8_causal_conv.restype = _I
+    L.ssdi8_causal_conv_step.argtypes = [i64, i64, ctypes.POINTER(ConvArgs), _P]
+    L.ssdi8_causal_conv_step.restype = _I
+    scan = [ctypes.POINTER(SelScanDims), ctypes.POINTER(SelScanArgs), _P]
+    L.ssdi8_selective_scan_workspace_size.argtypes = scan[:1]
+    L.ssdi8_selective_scan_workspace_size.restype = ctypes.c_size_t
+    L.ssdi8_selective_scan.argtypes = scan
+    L.ssdi8_selective_scan.restype = _I
+    L.ssdi8_selective_scan_step.argtypes = scan
+    L.ssdi8_selective_scan_step.restype = _I
+    L.ssdi8_gated_norm.argtypes = [i64, i64, i64, ctypes.POINTER(NormArgs), _P]
+    L.ssdi8_gated_norm.restype = _I
+    L.ssdi8_linear.argtypes = [i64, i64, i64, ctypes.POINTER(LinearArgs), _P]
+    L.ssdi8_linear.restype = _I
     L.ssdi8_status_string.argtypes = [_I]
     L.ssdi8_status_string.restype = ctypes.c_char_p
     L.ssdi8_version.argtypes = []
@@ -619,6 +679,320 @@ def decode_step(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bq: torch.Te
     st = lib().ssdi8_decode_step(B, H, P, G, N, ctypes.byref(a), _stream(stream))
     _check(st, "ssdi8_decode_step")
     return out
+
+
+# ------------------------------------------------------------------- around the layer in a block
+_DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
+_ACTIVATIONS = (torch.float32, torch.float16, torch.bfloat16)
+
+
+def _on(stream):
+    """Where outputs and workspaces are allocated: on the stream that the call runs on, so that their
+    memory is not handed out again while it runs."""
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        raw = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+        stream = torch.cuda.ExternalStream(raw or 0)
+    return torch.cuda.stream(stream)
+
+
+def _dense(t: torch.Tensor, dims: int) -> bool:
+    """Whether the last `dims` dimensions are dense (sizes of 1 have any stride)."""
+    want = 1
+    for k in range(1, dims + 1):
+        if t.shape[-k] != 1 and t.stride(-k) != want:
+            return False
+        want *= t.shape[-k]
+    return True
+
+
+def _rows(t: torch.Tensor, name: str, dtype, shape, dense: int = 1) -> torch.Tensor:
+    """A device tensor of this type and shape whose last `dense` dimensions are dense."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    if t.numel() and not _dense(t, dense):
+        raise ValueError(f"{name}: its last {'dimension is' if dense == 1 else 'dimensions are'} not dense")
+    return t
+
+
+def _activation_type(t: torch.Tensor, name: str, dims: int) -> None:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dtype not in _ACTIVATIONS:
+        raise ValueError(f"unsupported dtype {t.dtype}")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
+
+
+def _param(t: Optional[torch.Tensor], name: str, shape) -> Optional[int]:
+    return None if t is None else _ptr(_need(t, name, torch.float32, shape))
+
+
+def _act(name, allowed) -> int:
+    if name not in ACT or ACT[name] not in allowed:
+        raise ValueError(f"unknown activation {name!r}")
+    return ACT[name]
+
+
+def _conv(x, weight, bias, activation, split, y, B, L, stream):
+    """The arguments that the two convolutions share, and the outputs (batch and tokens, columns)."""
+    D = x.shape[-1]
+    if weight.dim() != 2:
+        raise ValueError("weight must be (channels, width)")
+    a = ConvArgs()
+    a.dtype, a.x, a.x_batch_stride = _DTYPES[x.dtype], _ptr(x), x.stride(0)
+    a.weight, a.width = _param(weight, "weight", (D, weight.shape[1])), weight.shape[1]
+    a.bias = _param(bias, "bias", (D,))
+    a.act = _act(activation, (0, 1))
+    cols = (D,) if split is None else tuple(int(c) for c in split)
+    if not 1 <= len(cols) <= 3 or min(cols) < 0 or sum(cols) != D:
+        raise ValueError(f"split must be up to three sizes that add up to {D}")
+    lead = tuple(x.shape[:-1])
+    if y is None:
+        with _on(stream):
+            y = tuple(torch.empty(*lead, c, dtype=x.dtype, device=x.device) for c in cols)
+    else:
+        y = (y,) if isinstance(y, torch.Tensor) else tuple(y)
+        if len(y) != len(cols):
+            raise ValueError(f"{len(cols)} outputs are needed")
+        for t, c in zip(y, cols):
+            _need(t, "y", x.dtype, (*lead, c))
+    for i, (t, c) in enumerate(zip(y, cols)):
+        a.y[i], a.y_cols[i] = _ptr(t), c
+    return a, y
+
+
+def causal_conv(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torch.Tensor] = None,
+                activation: Optional[str] = "silu", split=None,
+                init_state: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                y=None, final_state: bool = True, stream=None) -> Dict[str, object]:
+    """The short causal convolution in front of a scan (ssdi8_causal_conv): x (B,L,D) with dense
+    rows at any strides, weight (D,W) fp32 with W 2 to 4, bias (D), activation "silu" or None,
+    init_state (B,W-1,D) the inputs before the first token, lengths (B) int32.
+    split: up to three column counts; y is then a tuple of dense tensors, e.g. x, B, C of the layer.
+    Returns y and, with final_state, the last W-1 inputs (B,W-1,D)."""
+    _activation_type(x, "x", 3)
+    B, L, D = x.shape
+    _rows(x, "x", x.dtype, (B, L, D))
+    a, out = _conv(x, weight, bias, activation, split, y, B, L, stream)
+    a.x_token_stride = x.stride(1)
+    W = a.width
+    if init_state is not None:
+        a.init_state = _ptr(_need(init_state, "init_state", x.dtype, (B, W - 1, D)))
+    if lengths is not None:
+        a.lengths = _ptr(_need(lengths, "lengths", torch.int32, (B,)))
+    res: Dict[str, object] = {"y": out[0] if split is None else out}
+    if final_state:
+        with _on(stream):
+            res["final_state"] = torch.empty(B, max(W - 1, 0), D, dtype=x.dtype, device=x.device)
+        a.final_state = _ptr(res["final_state"])
+    _check(lib().ssdi8_causal_conv(B, L, D, ctypes.byref(a), _stream(stream)), "ssdi8_causal_conv")
+    return res
+
+
+def causal_conv_step(x: torch.Tensor, weight: torch.Tensor, state: torch.Tensor, *,
+                     bias: Optional[torch.Tensor] = None, activation: Optional[str] = "silu",
+                     split=None, y=None, stream=None):
+    """One token of causal_conv (ssdi8_causal_conv_step): x (B,D); state (B,W-1,D), the inputs before the
+    token, is updated in place.  Returns y (B,D), or the tuple of its columns with split."""
+    _activation_type(x, "x", 2)
+    B, D = x.shape
+    _rows(x, "x", x.dtype, (B, D))
+    a, out = _conv(x, weight, bias, activation, split, y, B, 1, stream)
+    a.final_state = _ptr(_need(state, "state", x.dtype, (B, a.width - 1, D)))
+    _check(lib().ssdi8_causal_conv_step(B, D, ctypes.byref(a), _stream(stream)),
+           "ssdi8_causal_conv_step")
+    return out[0] if split is None else out
+
+
+def _sel_scan(u, dt, A, B, C, D, z, dt_bias, dt_softplus, y, stream):
+    """The arguments that the two selective scans share, their sizes, and y."""
+    lead, ch = tuple(u.shape[:-1]), u.shape[-1]
+    H = dt.shape[-1] if dt.dim() == u.dim() else 0
+    if H < 1 or ch % H:
+        raise ValueError("dt must have a column per head (heads of equal size)")
+    if B.dim() != u.dim() + 1:
+        raise ValueError("B and C must be (..., groups, states)")
+    G, N = B.shape[-2], B.shape[-1]
+    d = SelScanDims(lead[0], lead[1] if len(lead) == 2 else 1, H, ch // H, G, N)
+    a = SelScanArgs()
+    a.dtype = _DTYPES[u.dtype]
+    if dt.dtype not in (torch.float32, u.dtype):
+        raise ValueError(f"dt must be torch.float32 or {u.dtype}, got {dt.dtype}")
+    a.dt_dtype = _DTYPES[dt.dtype]
+    named = (("u", _rows(u, "u", u.dtype, (*lead, ch))), ("dt", _rows(dt, "dt", dt.dtype, (*lead, H))),
+             ("B", _rows(B, "B", u.dtype, (*lead, G, N), 2)),
+             ("C", _rows(C, "C", u.dtype, (*lead, G, N), 2)),
+             ("z", None if z is None else _rows(z, "z", u.dtype, (*lead, ch))))
+    for name, t in named:
+        if t is not None:
+            setattr(a, name, _ptr(t))
+            setattr(a, name + "_batch_stride", t.stride(0))
+            if len(lead) == 2:
+                setattr(a, name + "_token_stride", t.stride(1))
+    a.tied = int(A.dim() == 1)
+    a.A = _param(A, "A", (H,) if a.tied else (ch, N))
+    a.D, a.dt_bias = _param(D, "D", (H,)), _param(dt_bias, "dt_bias", (H,))
+    a.dt_softplus = int(dt_softplus)
+    if y is None:
+        with _on(stream):
+            y = torch.empty(*lead, ch, dtype=u.dtype, device=u.device)
+    a.y = _ptr(_need(y, "y", u.dtype, (*lead, ch)))
+    return d, a, y
+
+
+def selective_scan(u: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                   C: torch.Tensor, *, D: Optional[torch.Tensor] = None,
+                   z: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None,
+                   dt_softplus: bool = True, init_state: Optional[torch.Tensor] = None,
+                   lengths: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
+                   final_state: bool = True, workspace: Optional[torch.Tensor] = None,
+                   stream=None) -> Dict[str, torch.Tensor]:
+    """The selective state space scan at any length (ssdi8_selective_scan).  u, z (b,L,ch), dt (b,L,H) of
+    u's type or fp32 with ch a multiple of H, A (ch,N) or, one decay per head, (H); B, C (b,L,G,N),
+    D, dt_bias (H), init_state (b,ch,N) fp32, lengths (b) int32.  Rows are dense, their strides any.
+    Returns y (b,L,ch) and, with final_state, the state after the last token (b,ch,N) fp32."""
+    _activation_type(u, "u", 3)
+    d, a, y = _sel_scan(u, dt, A, B, C, D, z, dt_bias, dt_softplus, y, stream)
+    state = (d.batch, u.shape[2], d.dstate)
+    if init_state is not None:
+        a.init_state = _param(init_state, "init_state", state)
+    if lengths is not None:
+        a.lengths = _ptr(_need(lengths, "lengths", torch.int32, (d.batch,)))
+    out = {"y": y}
+    need = selective_scan_workspace_size(d)
+    with _on(stream):
+        if final_state:
+            out["final_state"] = torch.empty(state, dtype=torch.float32, device=u.device)
+            a.final_state = _ptr(out["final_state"])
+        if workspace is None and need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=u.device)
+    if workspace is not None:
+        _need(workspace, "workspace", torch.uint8)
+        a.workspace, a.workspace_bytes = _ptr(workspace), workspace.numel()
+    _check(lib().ssdi8_selective_scan(ctypes.byref(d), ctypes.byref(a), _stream(stream)),
+           "ssdi8_selective_scan")
+    return out
+
+
+def selective_scan_workspace_size(d: SelScanDims) -> int:
+    return int(lib().ssdi8_selective_scan_workspace_size(ctypes.byref(d)))
+
+
+def selective_scan_step(u: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.Tensor,
+                        C: torch.Tensor, state: torch.Tensor, *, D: Optional[torch.Tensor] = None,
+                        z: Optional[torch.Tensor] = None, dt_bias: Optional[torch.Tensor] = None,
+                        dt_softplus: bool = True, y: Optional[torch.Tensor] = None,
+                        stream=None) -> torch.Tensor:
+    """One token of selective_scan (ssdi8_selective_scan_step): u, z (b,ch), dt (b,H), B, C (b,G,N); state
+    (b,ch,N) fp32 is updated in place.  Returns y (b,ch)."""
+    _activation_type(u, "u", 2)
+    d, a, y = _sel_scan(u, dt, A, B, C, D, z, dt_bias, dt_softplus, y, stream)
+    a.final_state = _param(state, "state", (d.batch, u.shape[1], d.dstate))
+    _check(lib().ssdi8_selective_scan_step(ctypes.byref(d), ctypes.byref(a), _stream(stream)),
+           "ssdi8_selective_scan_step")
+    return y
+
+
+def _flat(t: torch.Tensor, name: str) -> torch.Tensor:
+    """The rows of (..., D) as (rows, D), without a copy."""
+    if not isinstance(t, torch.Tensor) or t.dim() < 2:
+        raise ValueError(f"{name} must be a tensor of rows")
+    if t.dim() == 2:
+        return t
+    try:
+        return t.view(-1, t.shape[-1]) if t.numel() else t.reshape(-1, t.shape[-1])
+    except RuntimeError:
+        raise ValueError(f"{name}: its rows do not lie at one stride") from None
+
+
+def gated_norm(x: torch.Tensor, weight: torch.Tensor, *, z: Optional[torch.Tensor] = None,
+               residual: Optional[torch.Tensor] = None, eps: float = 1e-5, groups: int = 1,
+               norm_before_gate: bool = False, y: Optional[torch.Tensor] = None,
+               residual_out: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """RMS norm with an optional gate and residual (ssdi8_gated_norm): x, z, residual (..., D), weight
+    (D); x and z may be columns of wider rows.  Returns y and, with a residual, the sum x + residual
+    (in residual_out, which may be the residual itself, or a new tensor)."""
+    lead = tuple(x.shape[:-1])
+    xr = _flat(x, "x")
+    _activation_type(xr, "x", 2)
+    M, D = xr.shape
+    _rows(xr, "x", x.dtype, (M, D))
+    a = NormArgs()
+    a.dtype, a.x, a.x_row_stride = _DTYPES[x.dtype], _ptr(xr), xr.stride(0)
+    if z is not None:
+        zr = _rows(_flat(z, "z"), "z", x.dtype, (M, D))
+        a.z, a.z_row_stride = _ptr(zr), zr.stride(0)
+    a.weight = _param(weight, "weight", (D,))
+    a.eps, a.norm_before_gate = float(eps), int(norm_before_gate)
+    with _on(stream):
+        if y is None:
+            y = torch.empty(*lead, D, dtype=x.dtype, device=x.device)
+        if residual is not None and residual_out is None:
+            residual_out = torch.empty(*lead, D, dtype=x.dtype, device=x.device)
+    a.y = _ptr(_need(y, "y", x.dtype, (*lead, D)))
+    out = {"y": y}
+    if residual is not None:
+        a.residual = _ptr(_need(residual, "residual", x.dtype, (*lead, D)))
+        out["residual"] = residual_out
+    if residual_out is not None:
+        a.residual_out = _ptr(_need(residual_out, "residual_out", x.dtype, (*lead, D)))
+    _check(lib().ssdi8_gated_norm(M, D, int(groups), ctypes.byref(a), _stream(stream)),
+           "ssdi8_gated_norm")
+    return out
+
+
+def linear(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torch.Tensor] = None,
+           activation: Optional[str] = None, residual: Optional[torch.Tensor] = None,
+           x_scale: Optional[torch.Tensor] = None, w_scale: Optional[torch.Tensor] = None,
+           y_dtype: Optional[torch.dtype] = None, y: Optional[torch.Tensor] = None,
+           stream=None) -> torch.Tensor:
+    """A projection with its epilogue (ssdi8_linear): act(x weight^T + bias) + residual.  x (..., K) and
+    weight (O,K) fp16 or bf16, or int8 codes with x_scale (one step per row of x) and w_scale (O);
+    bias (O) fp32, activation None, "silu", "gelu" or "softplus", residual (..., O) of y's type.
+    y (..., O) has x's type (int8: fp16) or is fp32 (y_dtype)."""
+    lead = tuple(x.shape[:-1])
+    xr = _flat(x, "x")
+    if x.dtype not in (torch.float16, torch.bfloat16, torch.int8):
+        raise ValueError(f"unsupported dtype {x.dtype}")
+    M, K = xr.shape
+    _rows(xr, "x", x.dtype, (M, K))
+    if weight.dim() != 2:
+        raise ValueError("weight must be (outputs, inputs)")
+    O = weight.shape[0]
+    _rows(weight, "weight", x.dtype, (O, K))
+    quantized = x.dtype == torch.int8
+    if quantized != (x_scale is not None) or quantized != (w_scale is not None):
+        raise ValueError("x_scale and w_scale belong to int8 x and weight")
+    a = LinearArgs()
+    a.dtype, a.x, a.x_row_stride = _DTYPES[x.dtype], _ptr(xr), xr.stride(0)
+    a.weight, a.weight_row_stride = _ptr(weight), weight.stride(0)
+    if quantized:
+        if x_scale.numel() != M:
+            raise ValueError(f"x_scale must have {M} elements")
+        a.x_scale = _ptr(_need(x_scale, "x_scale", torch.float32))
+        a.weight_scale = _param(w_scale, "w_scale", (O,))
+    a.bias = _param(bias, "bias", (O,))
+    a.act = _act(activation, (0, 1, 2, 3))
+    own = torch.float16 if quantized else x.dtype
+    y_dtype = (own if y is None else y.dtype) if y_dtype is None else y_dtype
+    if y_dtype not in (torch.float32, own):
+        raise ValueError(f"y must be torch.float32 or {own}, got {y_dtype}")
+    if y is None:
+        with _on(stream):
+            y = torch.empty(*lead, O, dtype=y_dtype, device=x.device)
+    yr = _rows(_flat(y, "y"), "y", y_dtype, (M, O))
+    a.y, a.y_row_stride, a.y_dtype = _ptr(yr), max(yr.stride(0), O) if M <= 1 else yr.stride(0), _DTYPES[y_dtype]
+    if residual is not None:
+        rr = _rows(_flat(residual, "residual"), "residual", y_dtype, (M, O))
+        a.residual, a.residual_row_stride = _ptr(rr), rr.stride(0)
+    _check(lib().ssdi8_linear(M, O, K, ctypes.byref(a), _stream(stream)), "ssdi8_linear")
+    return y
 
 
 class SSDi8Layer:
