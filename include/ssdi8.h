@@ -465,6 +465,7 @@ ssdi8_status ssdi8_gated_norm(int64_t rows, int64_t channels, int64_t groups,
  * with s = 1 (fp16, bf16: products in fp32) or x_scale[r] weight_scale[o] (int8: products in int32; the
  * codes and per-token steps of ssdi8_quantize_act with SSDI8_GRAN_TOKEN, and weights quantized per
  * output).  y and the residual are fp32 or x's type (int8: fp16).  k >= 1, up to 131072 for int8.
+ * 256 rows of x, and of weight, span less than 4e9 bytes.
  */
 typedef struct {
   int dtype;                                /* of x and weight: SSDI8_F16, SSDI8_BF16, SSDI8_I8   */

@@ -214,6 +214,10 @@ ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_
   if (bad_stride(a->x_row_stride) || bad_stride(a->weight_row_stride) ||
       bad_stride(a->residual_row_stride) || a->y_row_stride < outputs || bad_stride(a->y_row_stride))
     return SSDI8_ERR_SHAPE;
+  const int64_t x_row = rows > 1 ? a->x_row_stride : 0;
+  const int64_t w_row = outputs > 1 ? a->weight_row_stride : 0;
+  if ((255.0 * (double)(x_row > w_row ? x_row : w_row) + (double)k) * (double)size_of(a->dtype) > 4.0e9)
+    return SSDI8_ERR_UNSUPPORTED;   // the kernels take 256 rows with 32-bit offsets
   if (rows == 0) return SSDI8_OK;
   if (!a->x || !a->weight || !a->y || (quantized && (!a->x_scale || !a->weight_scale)))
     return SSDI8_ERR_NULL;
@@ -230,8 +234,8 @@ ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_
   l.k = k;
   l.x = a->x;
   l.w = a->weight;
-  l.x_row = a->x_row_stride;
-  l.w_row = a->weight_row_stride;
+  l.x_row = x_row;
+  l.w_row = w_row;
   l.x_scale = a->x_scale;
   l.w_scale = a->weight_scale;
   l.bias = a->bias;

@@ -4,17 +4,16 @@
 // is 16 consecutive bytes of a row for every type: the kernels count k in bytes and differ by type only in
 // the instruction.
 //
-// Many rows (linear_tile): a workgroup forms a kBM x kBN tile of y from k-tiles of 128 bytes per row,
-// brought straight into LDS, two buffers deep: the loads of a k-tile are issued behind the barrier that
-// frees its buffer and have a whole tile's products to arrive.  LDS holds 16-byte chunk c of row r at slot
-// c ^ (r % 8), so that the 64 lanes of a fragment read touch every bank alike; the loads write LDS lane by
-// lane, so the exchange is made on the global address.  w is the first operand: a lane then holds four
-// consecutive columns of a row, and the tile leaves through LDS in whole lines.
+// Many rows (linear_tile): a workgroup forms a kBM x kBN tile of y from k-tiles of 128 bytes per row in two
+// LDS buffers, a third k-tile on its way in registers.  LDS holds 16-byte chunk c of row r at slot
+// c ^ (r / 2 % 8), so that the 16 lanes that a fragment read serves at a time touch every bank once.  w is
+// the first operand: a lane then holds four consecutive columns of a row, and the tile leaves through LDS
+// in whole lines.
 // Few rows (linear_rows): bound by the bytes of w.  A workgroup takes 16 rows of w, its waves share k by
 // lines of 128 bytes, each straight from memory into the matrix instruction's registers, and their sums
 // meet in LDS.
-// A row's end inside a k-tile, and rows that do not start at multiples of 16 bytes, go through registers,
-// where what lies behind the end becomes 0 in both operands.
+// What lies behind a row's end in its last k-tile or line becomes 0 in both operands; rows may start at any
+// element.
 #include <type_traits>
 
 #include "block.hpp"
@@ -71,7 +70,8 @@ struct I8 {
   }
 };
 
-constexpr int kLine = 128;   // bytes of k per k-tile
+constexpr int kLine = 128;    // bytes of k per k-tile
+constexpr int kChunks = kLine / 16;
 
 // Bytes [at, at + 16) of a row of `bytes`, 0 behind its end; at any alignment of an element.
 template <typename T> __device__ __forceinline__ uint4 load_chunk(const char* row, int64_t at, int64_t bytes) {
@@ -119,13 +119,12 @@ __device__ __forceinline__ void finish_vec(const LinearArgs& a, int64_t m, int64
     store_vec<Out>(static_cast<Out*>(a.y) + m * a.y_row + c, n, v);
 }
 
-typedef __attribute__((address_space(3))) void* LdsPtr;
-typedef const __attribute__((address_space(1))) void* GlobalPtr;
+// The exchange of chunks in LDS row r (see above).
+__device__ __forceinline__ int slot_key(int r) { return (r >> 1) & 7; }
 
 // kWM x kWN waves, each a (kBM / kWM) x (kBN / kWN) part of the tile.
 template <typename K, int kBM, int kBN, int kWM, int kWN>
-__global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int mtiles, int ntiles,
-                                                               int direct) {
+__global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int mtiles, int ntiles) {
   constexpr int kThreads = 64 * kWM * kWN;
   constexpr int kTM = kBM / kWM / 32, kTN = kBN / kWN / 32;
   constexpr int kBuf = (kBM + kBN) * kLine;
@@ -136,133 +135,173 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave / kWN, wn = wave % kWN;
-  // tiles of one XCD lie together: bands of eight rows of tiles, column by column
+  // tiles of one XCD lie together: bands of four rows of tiles, column by column
   const int id = xcd_remap(blockIdx.x, mtiles * ntiles);
-  constexpr int kBand = 8;
+  constexpr int kBand = 4;
   const int band = id / (kBand * ntiles), in = id % (kBand * ntiles);
   const int rows = mtiles - band * kBand < kBand ? mtiles - band * kBand : kBand;
   const int64_t m0 = (int64_t)(band * kBand + in % rows) * kBM;
   const int64_t n0 = (int64_t)(in / rows) * kBN;
 
   const int64_t kbytes = a.k * (int64_t)sizeof(T);
-  const int ktiles = (int)((kbytes + kLine - 1) / kLine);
-  const char* xp = static_cast<const char*>(a.x);
-  const char* wp = static_cast<const char*>(a.w);
-
-  // this thread's part of a k-tile: chunk `slot` of LDS row r = i * kThreads / 8 + tid / 8 holds chunk
-  // slot ^ (r % 8) of that row
-  constexpr int kA = kBM * 8 / kThreads, kB = kBN * 8 / kThreads;
-  static_assert(kThreads % 64 == 0 && kBM * 8 % kThreads == 0 && kBN * 8 % kThreads == 0, "tile");
-  const int lrow = tid >> 3, chunk = (tid & 7) ^ (lrow & 7);
-  const char *ap[kA], *bp[kB];
+  const int whole = (int)(kbytes / kLine), ktiles = (int)((kbytes + kLine - 1) / kLine);
+  // this thread's part of a k-tile: slot tid % kChunks of LDS row r = i * kThreads / kChunks + tid / kChunks
+  // holds chunk slot ^ key(r) of that row
+  constexpr int kLoadRows = kThreads / kChunks;
+  constexpr int kA = kBM / kLoadRows, kB = kBN / kLoadRows;
+  static_assert(kLoadRows % 16 == 0 && kBM % kLoadRows == 0 && kBN % kLoadRows == 0, "tile");
+  const int lrow = tid / kChunks, chunk = (tid % kChunks) ^ slot_key(lrow);
+  // rows behind the last are taken for it: their results are not stored.  32-bit offsets from the tile's
+  // first row (the host refuses rows too far apart for them)
+  uint32_t offset[kA + kB];
 #pragma unroll
-  for (int i = 0; i < kA; ++i) {
-    int64_t r = m0 + i * (kThreads / 8) + lrow;
-    r = r < a.m ? r : a.m - 1;   // rows behind the last: their results are not stored
-    ap[i] = xp + r * a.x_row * (int64_t)sizeof(T);
+  for (int i = 0; i < kA + kB; ++i) {
+    const int64_t left = i < kA ? a.m - m0 : a.n - n0;
+    int64_t r = (i < kA ? i : i - kA) * kLoadRows + lrow;
+    r = r < left ? r : left - 1;
+    offset[i] = (uint32_t)(r * (i < kA ? a.x_row : a.w_row) * (int64_t)sizeof(T)) + chunk * 16;
   }
-#pragma unroll
-  for (int i = 0; i < kB; ++i) {
-    int64_t r = n0 + i * (kThreads / 8) + lrow;
-    r = r < a.n ? r : a.n - 1;
-    bp[i] = wp + r * a.w_row * (int64_t)sizeof(T);
-  }
-  auto fetch = [&](int kt) {
-    char* buf = lds + (kt & 1) * kBuf;
-    const int64_t at = (int64_t)kt * kLine + chunk * 16;
-    if (direct && (int64_t)(kt + 1) * kLine <= kbytes) {
-#pragma unroll
-      for (int i = 0; i < kA; ++i)
-        __builtin_amdgcn_global_load_lds((GlobalPtr)(ap[i] + at),
-                                         (LdsPtr)(buf + (i * kThreads + wave * 64) * 16), 16, 0, 0);
-#pragma unroll
-      for (int i = 0; i < kB; ++i)
-        __builtin_amdgcn_global_load_lds(
-            (GlobalPtr)(bp[i] + at), (LdsPtr)(buf + kBM * kLine + (i * kThreads + wave * 64) * 16), 16,
-            0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kA; ++i)
-        *reinterpret_cast<uint4*>(buf + (i * kThreads + tid) * 16) = load_chunk<T>(ap[i], at, kbytes);
-#pragma unroll
-      for (int i = 0; i < kB; ++i)
-        *reinterpret_cast<uint4*>(buf + kBM * kLine + (i * kThreads + tid) * 16) =
-            load_chunk<T>(bp[i], at, kbytes);
-    }
-  };
+  const char* xp = static_cast<const char*>(a.x) + m0 * a.x_row * (int64_t)sizeof(T);
+  const char* wp = static_cast<const char*>(a.w) + n0 * a.w_row * (int64_t)sizeof(T);
 
   typename K::Acc32 acc[kTN][kTM] = {};
   const int fr = lane & 31, fk = lane >> 5;
   const int arow = (wm * kTM * 32 + fr) * kLine, brow = kBM * kLine + (wn * kTN * 32 + fr) * kLine;
-  fetch(0);
-  for (int kt = 0; kt < ktiles; ++kt) {
-    // this wave's loads have arrived, every wave has read the other buffer
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  struct Frags {
+    uint4 x[kTM], w[kTN];
+  };
+  auto read = [&](int kt, int ks, Frags& f) {
+    const char* buf = lds + kt % 2 * kBuf;
+    const int off = ((2 * ks + fk) ^ slot_key(fr)) * 16;
+#pragma unroll
+    for (int i = 0; i < kTM; ++i)
+      f.x[i] = *reinterpret_cast<const uint4*>(buf + arow + i * 32 * kLine + off);
+#pragma unroll
+    for (int i = 0; i < kTN; ++i)
+      f.w[i] = *reinterpret_cast<const uint4*>(buf + brow + i * 32 * kLine + off);
+  };
+  // One 16-byte load per lane of a k-tile on its way, and its place in LDS.
+  constexpr int kParts = kA + kB;
+  uint4 part[kParts];
+  auto request = [&](int kt, int i, auto inside) {   // inside: a whole k-tile
+    const char* p = (i < kA ? xp : wp) + (int64_t)kt * kLine + offset[i];
+    if constexpr (decltype(inside)::value) __builtin_memcpy(&part[i], p, 16);
+    else part[i] = load_chunk<T>(p, 0, kbytes - (int64_t)kt * kLine - chunk * 16);
+  };
+  auto put = [&](int kt, int i) {
+    char* buf = lds + (kt & 1) * kBuf + (i < kA ? 0 : kBM * kLine) + tid * 16;
+    *reinterpret_cast<uint4*>(buf + (i < kA ? i : i - kA) * kThreads * 16) = part[i];
+  };
+  // Step ks of k-tile kt forms the products of 32 bytes.  Meanwhile the next step's fragments are read,
+  // over the k-tiles' borders too, and the next k-tile moves from registers to the other buffer, a part
+  // per step, each part's registers taking the k-tile after it: a load has four steps to arrive, and no
+  // step waits for the address unit, which takes as long for a k-tile's 64 KB as two steps' products.
+  constexpr int kSteps = kLine / 32, kPerStep = (kParts + kSteps - 2) / (kSteps - 1);
+  Frags f[2];
+  auto begin = [&](auto inside) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) request(0, i, inside);
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) put(0, i);
+    if (decltype(inside)::value || ktiles > 1)
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) request(1, i, inside);
     __syncthreads();
-    if (kt + 1 < ktiles) fetch(kt + 1);
-    const char* buf = lds + (kt & 1) * kBuf;
+    read(0, 0, f[0]);
+  };
+  auto k_tile = [&](int kt, auto inside) {   // inside: k-tiles kt + 1 and kt + 2 are there and whole
+    constexpr bool kInside = decltype(inside)::value;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const int off = ((2 * ks + fk) ^ (fr & 7)) * 16;
-      uint4 av[kTM], bv[kTN];
+    for (int ks = 0; ks < kSteps; ++ks) {
+      if (ks + 1 < kSteps) {
+        read(kt, ks + 1, f[(ks + 1) & 1]);
+      } else if (kInside || kt + 1 < ktiles) {
+        __syncthreads();   // the next buffer is written, this one read
+        read(kt + 1, 0, f[0]);
+      }
 #pragma unroll
-      for (int i = 0; i < kTM; ++i)
-        av[i] = *reinterpret_cast<const uint4*>(buf + arow + i * 32 * kLine + off);
+      for (int j = 0; j < kTN; ++j) {
 #pragma unroll
-      for (int i = 0; i < kTN; ++i)
-        bv[i] = *reinterpret_cast<const uint4*>(buf + brow + i * 32 * kLine + off);
+        for (int i = 0; i < kTM; ++i)
+          acc[j][i] = K::mma32(f[ks & 1].w[j], f[ks & 1].x[i], acc[j][i]);
+        // the compiler would otherwise gather the loads at the end of the k-tile
+        __builtin_amdgcn_sched_barrier(0);
+        if (j == 0 && ks + 1 < kSteps && (kInside || kt + 1 < ktiles)) {
 #pragma unroll
-      for (int j = 0; j < kTN; ++j)
-#pragma unroll
-        for (int i = 0; i < kTM; ++i) acc[j][i] = K::mma32(bv[j], av[i], acc[j][i]);
+          for (int e = 0; e < kPerStep; ++e) {
+            const int i = ks * kPerStep + e;
+            if (i < kParts) {
+              put(kt + 1, i);
+              if (kInside || kt + 2 < ktiles) request(kt + 2, i, inside);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
     }
+  };
+  int kt = 0;
+  if (whole > 2) {
+    begin(std::true_type());
+    for (; kt + 2 < whole; ++kt) k_tile(kt, std::true_type());
+  } else {
+    begin(std::false_type());
   }
+  for (; kt < ktiles; ++kt) k_tile(kt, std::false_type());
   __syncthreads();
 
-  // a lane holds row fr of the 32 x 32 block, columns 8 q + 4 fk + (0..3)
+  // a lane holds row fr of the 32 x 32 block, columns 8 q + 4 fk + (0..3); on the way out it has eight
+  // columns, the same ones of every row
   float* out = reinterpret_cast<float*>(lds) + wave * 32 * kOutRow;
   const int64_t wm0 = m0 + wm * kTM * 32, wn0 = n0 + wn * kTN * 32;
   constexpr int kPer = kTN * 32 / kVec;    // lanes of a row on the way out
   constexpr int kRows = 64 / kPer;
+  const int oc = (lane % kPer) * kVec;
+  const int64_t cc = wn0 + oc;
+  const int cn = cc >= a.n ? 0 : (a.n - cc < kVec ? (int)(a.n - cc) : kVec);
+  float bias[kVec] = {}, ws[kVec] = {};
+  if (a.bias) load_vec<float>(a.bias + cc, cn, bias);
+  if constexpr (std::is_same_v<K, I8>) load_vec<float>(a.w_scale + cc, cn, ws);
 #pragma unroll
   for (int i = 0; i < kTM; ++i) {
-    const int64_t m = wm0 + i * 32 + fr;
-    float sx = 1.0f;
-    if constexpr (std::is_same_v<K, I8>) sx = a.x_scale[m < a.m ? m : a.m - 1];
 #pragma unroll
     for (int j = 0; j < kTN; ++j)
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int64_t n = wn0 + j * 32 + 8 * q + 4 * fk + e;
-          const int64_t nn = n < a.n ? n : a.n - 1;
-          v[e] = (float)acc[j][i][4 * q + e];
-          if constexpr (std::is_same_v<K, I8>) v[e] *= sx * a.w_scale[nn];
-          if (a.bias) v[e] += a.bias[nn];
-          if (a.act) v[e] = activate(v[e], a.act);
-        }
+      for (int q = 0; q < 4; ++q)
         *reinterpret_cast<float4*>(out + fr * kOutRow + j * 32 + 8 * q + 4 * fk) =
-            make_float4(v[0], v[1], v[2], v[3]);
-      }
+            make_float4((float)acc[j][i][4 * q], (float)acc[j][i][4 * q + 1],
+                        (float)acc[j][i][4 * q + 2], (float)acc[j][i][4 * q + 3]);
     // the wave's own rows: no other wave reads or writes them
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int r0 = 0; r0 < 32; r0 += kRows) {
-      const int r = r0 + lane / kPer, c = (lane % kPer) * kVec;
-      const int64_t mm = wm0 + i * 32 + r, cc = wn0 + c;
+      const int r = r0 + lane / kPer;
+      const int64_t mm = wm0 + i * 32 + r;
       float v[kVec];
-      const float4 lo = *reinterpret_cast<const float4*>(out + r * kOutRow + c);
-      const float4 hi = *reinterpret_cast<const float4*>(out + r * kOutRow + c + 4);
+      const float4 lo = *reinterpret_cast<const float4*>(out + r * kOutRow + oc);
+      const float4 hi = *reinterpret_cast<const float4*>(out + r * kOutRow + oc + 4);
       v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
       v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
-      if (mm < a.m && cc < a.n)
-        finish_vec<typename K::Out>(a, mm, cc, a.n - cc < kVec ? (int)(a.n - cc) : kVec, v);
+      if (mm < a.m && cn > 0) {
+        if constexpr (std::is_same_v<K, I8>) {
+          const float sx = a.x_scale[mm];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) v[e] *= sx * ws[e];
+        }
+        if (a.bias)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) v[e] += bias[e];
+        if (a.act)
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) v[e] = activate(v[e], a.act);
+        finish_vec<typename K::Out>(a, mm, cc, cn, v);
+      }
     }
     __builtin_amdgcn_wave_barrier();
   }
 }
+
+constexpr int kRowLine = 128;
 
 // 16 rows of w by kMT x 16 rows of x per workgroup of kWaves waves.
 template <typename K, int kMT, int kWaves>
@@ -273,7 +312,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows(LinearArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * kMT);
   const int64_t kbytes = a.k * (int64_t)sizeof(T);
-  const int lines = (int)((kbytes + kLine - 1) / kLine);
+  const int lines = (int)((kbytes + kRowLine - 1) / kRowLine);
   const int fr = lane & 15, fk = lane >> 4;
   const int64_t wr = n0 + fr < a.n ? n0 + fr : a.n - 1;
   const char* wrow = static_cast<const char*>(a.w) + wr * a.w_row * (int64_t)sizeof(T);
@@ -288,7 +327,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows(LinearArgs a) {
   for (int l = wave; l < lines; l += kWaves) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int64_t at = (int64_t)l * kLine + s * 64 + fk * 16;
+      const int64_t at = (int64_t)l * kRowLine + s * 64 + fk * 16;
       const uint4 wv = load_chunk<T>(wrow, at, kbytes);
 #pragma unroll
       for (int i = 0; i < kMT; ++i)
@@ -324,10 +363,10 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows(LinearArgs a) {
 }
 
 template <typename K, int kBM, int kBN, int kWM, int kWN>
-hipError_t run_tile(const LinearArgs& a, int direct, hipStream_t st) {
+hipError_t run_tile(const LinearArgs& a, hipStream_t st) {
   const int64_t mt = (a.m + kBM - 1) / kBM, nt = (a.n + kBN - 1) / kBN;
   linear_tile<K, kBM, kBN, kWM, kWN>
-      <<<dim3((unsigned)(mt * nt)), 64 * kWM * kWN, 0, st>>>(a, (int)mt, (int)nt, direct);
+      <<<dim3((unsigned)(mt * nt)), 64 * kWM * kWN, 0, st>>>(a, (int)mt, (int)nt);
   return hipGetLastError();
 }
 
@@ -339,13 +378,27 @@ template <typename K> hipError_t run(const LinearArgs& a, hipStream_t st) {
     else linear_rows<K, 4, 8><<<dim3(nt, 1), 512, 0, st>>>(a);
     return hipGetLastError();
   }
-  constexpr int64_t es = sizeof(typename K::T);
-  const int direct = ((uintptr_t)a.x % 16 == 0 && (uintptr_t)a.w % 16 == 0 &&
-                      a.x_row * es % 16 == 0 && a.w_row * es % 16 == 0);
-  auto tiles = [&](int64_t bm, int64_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
-  if (tiles(256, 256) >= 256) return run_tile<K, 256, 256, 2, 4>(a, direct, st);
-  if (tiles(128, 128) >= 128) return run_tile<K, 128, 128, 2, 2>(a, direct, st);
-  return run_tile<K, 64, 64, 2, 2>(a, direct, st);
+  // The tile whose rounds over the card's 256 CUs cost least: rounds * area / rate, the rates (of the
+  // largest tile's) as 8192^3 in bf16 measured them: 898 us with 256 x 256, 986 with 256 x 192, 1030 with
+  // 256 x 128, 1108 with 128 x 128, 1700 with 64 x 64.  Where another than the largest wins: 16384 x 768 x
+  // 1536 49.7 / 47.2 us with 256 x 192, 2048 x 2560 x 5120 104 / 68.7 with 256 x 128, 512 x 5120 x 2560
+  // 55.4 / 24.0 with 128 x 128, 128 x 5120 x 2560 54.2 / 16.5 with 64 x 64.
+  auto cost = [&](int64_t bm, int64_t bn, double rate) {
+    const int64_t tiles = ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn);
+    return (double)((tiles + 255) / 256) * (double)(bm * bn) / rate;
+  };
+  const double costs[] = {cost(256, 256, 1.0), cost(256, 192, 0.9), cost(256, 128, 0.87),
+                          cost(128, 128, 0.81), cost(64, 64, 0.53)};
+  int best = 0;
+  for (int i = 1; i < 5; ++i)
+    if (costs[i] < costs[best]) best = i;
+  switch (best) {
+    case 0: return run_tile<K, 256, 256, 2, 4>(a, st);
+    case 1: return run_tile<K, 256, 192, 4, 2>(a, st);
+    case 2: return run_tile<K, 256, 128, 4, 2>(a, st);
+    case 3: return run_tile<K, 128, 128, 2, 2>(a, st);
+    default: return run_tile<K, 64, 64, 2, 2>(a, st);
+  }
 }
 
 }  // namespace

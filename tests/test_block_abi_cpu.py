@@ -148,4 +148,6 @@ def test_linear(ssdi8):
     for n in ((-1, 32, 64), (3, 0, 64), (3, 32, 0), (1 << 31, 32, 64), (1 << 30, 1 << 13, 64)):
         assert call(changed(a, y_row_stride=1 << 20), n) == s.ERR_SHAPE, n
     assert call(a, (3, 32, 131073)) == s.ERR_UNSUPPORTED
+    assert call(changed(a, x_row_stride=1 << 24)) == s.ERR_UNSUPPORTED
+    assert call(changed(a, weight_row_stride=1 << 24)) == s.ERR_UNSUPPORTED
     assert call(a, (0, 32, 64)) == s.OK
