@@ -57,30 +57,37 @@ __device__ __forceinline__ float silu(float v) {
   return v * __builtin_amdgcn_rcpf(1.0f + fast_exp(-v));
 }
 // log(1 + exp(v)) in fp32, v itself above 20 (there the difference is below half an ulp).  With
-// z = exp(-|v|) and u = fl(1 + z), log(u) z / (u - 1) takes back the rounding of u.
+// z = exp(-|v|) and u = fl(1 + z), log(u) + (z - (u - 1)) takes back the rounding of u: the exact term is
+// (z - (u - 1)) / u, and what the missing division leaves is z (z - (u - 1)), below an ulp of the result.
 __device__ __forceinline__ float softplus_fast(float v) {
   const float z = fast_exp(-__builtin_fabsf(v));
-  const float u = 1.0f + z, d = u - 1.0f;
-  const float l = 0.693147180559945309f * __builtin_amdgcn_logf(u);   // log2
-  const float l1p = d == 0.0f ? z : l * (z * __builtin_amdgcn_rcpf(d));
-  const float s = v > 0.0f ? v + l1p : l1p;
-  return v > 20.0f ? v : s;
+  const float u = 1.0f + z;
+  const float l1p = __builtin_fmaf(0.693147180559945309f, __builtin_amdgcn_logf(u), z - (u - 1.0f));
+  const float s = __builtin_fmaxf(v, 0.0f) + l1p;
+  return v > 20.0f || v != v ? v : s;
 }
 
-// Sum over `kLanes` neighbouring lanes (a power of two), in every one of them.
-template <int kLanes> __device__ __forceinline__ float lane_sum(float v) {
-  auto dpp = [](float x, auto ctrl) {
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(
-                                         0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xf,
-                                         0xf, true));
+// Sums over kLanes neighbouring lanes (a power of two) of kCount values, in every one of the lanes.
+template <int kCtrl> __device__ __forceinline__ float dpp_add(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl,
+                                                                   0xf, 0xf, true));
+}
+template <int kLanes, int kCount> __device__ __forceinline__ void lane_sums(float (&v)[kCount]) {
+  auto each = [&](auto step) {
+#pragma unroll
+    for (int j = 0; j < kCount; ++j) v[j] = step(v[j]);
   };
-  if constexpr (kLanes >= 2) v += dpp(v, std::integral_constant<int, 0xB1>());   // quad: 1 0 3 2
-  if constexpr (kLanes >= 4) v += dpp(v, std::integral_constant<int, 0x4E>());   // quad: 2 3 0 1
-  if constexpr (kLanes >= 8) v += dpp(v, std::integral_constant<int, 0x141>());  // half-row mirror
-  if constexpr (kLanes >= 16) v += dpp(v, std::integral_constant<int, 0x140>()); // row mirror
-  if constexpr (kLanes >= 32) v += __shfl_xor(v, 16);
-  if constexpr (kLanes >= 64) v += __shfl_xor(v, 32);
-  return v;
+  if constexpr (kLanes >= 2) each([](float x) { return dpp_add<0xB1>(x); });    // quad: 1 0 3 2
+  if constexpr (kLanes >= 4) each([](float x) { return dpp_add<0x4E>(x); });    // quad: 2 3 0 1
+  if constexpr (kLanes >= 8) each([](float x) { return dpp_add<0x141>(x); });   // half-row mirror
+  if constexpr (kLanes >= 16) each([](float x) { return dpp_add<0x140>(x); });  // row mirror
+  if constexpr (kLanes >= 32) each([](float x) { return x + __shfl_xor(x, 16); });
+  if constexpr (kLanes >= 64) each([](float x) { return x + __shfl_xor(x, 32); });
+}
+template <int kLanes> __device__ __forceinline__ float lane_sum(float v) {
+  float one[1] = {v};
+  lane_sums<kLanes, 1>(one);
+  return one[0];
 }
 
 // ---------------------------------------------------------------------------- launches

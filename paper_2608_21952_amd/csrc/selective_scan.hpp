@@ -1,0 +1,446 @@
+// The selective scan's kernel over prompts (described in selective_scan.hip).
+#pragma once
+
+#include <type_traits>
+
+#include "block.hpp"
+
+namespace ssdi8 {
+
+namespace sel_scan {
+
+constexpr int kTile = 32;
+constexpr int kThreads = 256;
+
+// kVec elements as they lie in memory (8 words of fp32, 4 of a 16-bit type), turned into fp32 later.  A
+// whole vector is requested without a choice between ways of loading it: where ways met, the compiler
+// waited for the data.
+struct Raw {
+  uint32_t w[kVec];
+};
+__device__ __forceinline__ void request_raw(Raw& r, const char* p, int dtype) {
+  __builtin_memcpy(r.w, p, 16);
+  if (dtype == 0) __builtin_memcpy(r.w + 4, p + 16, 16);
+}
+// The first n elements, the others 0.
+__device__ __forceinline__ void request_part(Raw& r, const char* p, int dtype, int n) {
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) r.w[i] = 0;
+#pragma unroll
+  for (int i = 0; i < kVec; ++i)
+    if (i < n) {
+      if (dtype == 0) r.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
+      else r.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+    }
+}
+__device__ __forceinline__ uint32_t load_raw1(const void* base, int64_t off, int dtype) {
+  return dtype == 0 ? static_cast<const uint32_t*>(base)[off]
+                    : (uint32_t) static_cast<const uint16_t*>(base)[off];
+}
+__device__ __forceinline__ float as_float(uint32_t bits, int dtype) {
+  if (dtype == 0) return __builtin_bit_cast(float, bits);
+  if (dtype == 1) return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
+  return __builtin_bit_cast(float, bits << 16);
+}
+__device__ __forceinline__ void as_floats(const Raw& r, int dtype, float (&out)[kVec]) {
+  if (dtype == 0) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) out[i] = __builtin_bit_cast(float, r.w[i]);
+  } else if (dtype == 1) {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      out[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i / 2] >> (16 * (i & 1))));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kVec; ++i)
+      out[i] = __builtin_bit_cast(float, i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
+  }
+}
+__device__ __forceinline__ void store_as(void* base, int64_t off, int dtype, int n,
+                                         const float (&v)[kVec]) {
+  if (dtype == 0) store_vec<float>(static_cast<float*>(base) + off, n, v);
+  else if (dtype == 1) store_vec<_Float16>(static_cast<_Float16*>(base) + off, n, v);
+  else store_vec<bf16>(static_cast<bf16*>(base) + off, n, v);
+}
+
+// A in base 2; -inf (a decay of 0 for any positive delta) stays finite, so that delta = 0 gives 1.
+__device__ __forceinline__ float decay_rate(float A) {
+  const float a = A * kLog2eF;
+  return a == -__builtin_inff() ? -__FLT_MAX__ : a;
+}
+
+// States [n0, n0 + kS) of a row of N, 0 behind its end.
+template <int kS> __device__ __forceinline__ void load_states(const float* row, int n0, int N, float (&h)[kS]) {
+  if (n0 + kS <= N) {
+    __builtin_memcpy(h, row + n0, sizeof(h));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kS; ++i) h[i] = n0 + i < N ? row[n0 + i] : 0.0f;
+  }
+}
+template <int kS>
+__device__ __forceinline__ void store_states(float* row, int n0, int N, const float (&h)[kS]) {
+  if (n0 + kS <= N) {
+    __builtin_memcpy(row + n0, h, sizeof(h));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kS; ++i)
+      if (n0 + i < N) row[n0 + i] = h[i];
+  }
+}
+
+struct Args {
+  SelScan s;
+  int64_t span;          // tokens of a span (a multiple of kTile)
+  int spans, D;
+  int group_ch, group_tiles;   // channels of a group, workgroups that hold them
+};
+
+// The channels [first, end) of a workgroup: tiles do not cross from one group of B, C to the next.
+struct Tile {
+  int group, first, end;
+};
+__device__ __forceinline__ Tile tile_of(const Args& p, int ct, int channels) {
+  Tile t;
+  t.group = ct / p.group_tiles;
+  t.first = t.group * p.group_ch + (ct % p.group_tiles) * channels;
+  t.end = (t.group + 1) * p.group_ch;
+  return t;
+}
+
+// kType, kDt: the types of the activations and of dt, -1 where they are only known at run time.  kFast: dt
+// of a vector of channels is a vector (a decay per channel and state, headdim 1) or one head's (tied
+// decay, headdim and group sizes multiples of kVec), and groups and states fill vectors.  The other form
+// takes everything, element by element where it has to, and waits for its loads.
+// Workspace of a cut scan: states [b, spans, d, n] (0: the initial state, c + 1: span c's from zero),
+// then the spans' decays [b, spans, d].
+template <int kLanes, int kS, bool kTied, bool kStates, int kType, int kDt, bool kFast>
+__global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
+  constexpr int kCh = kThreads / kLanes;            // channels of a workgroup
+  constexpr int kN = kLanes * kS;                   // states, padded
+  constexpr int kGroup = kS > 4 ? 2 : 4, kPair = 2 * kGroup;
+  constexpr int kVecs = kCh / kVec;                 // vectors of a token's channels
+  constexpr int kBcVecs = kTile * (kN / kVec);      // vectors of a tile of B (or C)
+  constexpr int kBc = (kBcVecs + kThreads - 1) / kThreads;
+  static_assert(kCh % kVec == 0 && kVecs * kTile <= kThreads && kN % kVec == 0, "tile");
+  __shared__ __attribute__((aligned(16))) float s_du[kTile][kCh][2];   // delta (or decay), delta u
+  __shared__ __attribute__((aligned(16))) float s_B[kTile][kN];
+  __shared__ __attribute__((aligned(16))) float s_C[kStates ? 1 : kTile][kStates ? 4 : kN];
+
+  const SelScan& a = p.s;
+  const int dtype = kType >= 0 ? kType : a.dtype, dt_dtype = kDt >= 0 ? kDt : a.dt_dtype;
+  const int tid = threadIdx.x;
+  const int nctile = p.group_tiles * (int)a.ngroups;
+  const Tile tile = tile_of(p, (int)(blockIdx.x % nctile), kCh);
+  const int group = tile.group;
+  const int64_t rest = blockIdx.x / nctile;
+  const int nsp = kStates ? p.spans - 1 : p.spans;
+  const int span = (int)(rest % nsp);
+  const int64_t b = rest / nsp;
+  const int D = p.D, N = (int)a.dstate, P = (int)a.headdim;
+  const int64_t L = a.seqlen;
+  int64_t len = L;
+  if (a.lengths) len = a.lengths[b] < 0 ? 0 : (a.lengths[b] < L ? a.lengths[b] : L);
+  const int64_t t_begin = span * p.span;
+  const int64_t t_end = t_begin + p.span < L ? t_begin + p.span : L;
+
+  // the states of this lane
+  const int ch = tid / kLanes, sub = tid % kLanes, n0 = sub * kS;
+  const int d = tile.first + ch;
+  const bool live = d < tile.end;
+  float rate[kS], h[kS] = {};
+  float* ws_decay = a.workspace + a.batch * p.spans * D * N;
+  float* ws_state = a.workspace + (b * p.spans * D + d) * (int64_t)N;   // span 0
+  const int64_t ws_span = (int64_t)D * N;
+  const int64_t state_row = (b * D + d) * (int64_t)N;
+#pragma unroll
+  for (int i = 0; i < kS; ++i) rate[i] = 0.0f;
+  if (live) {
+    if constexpr (!kTied) {
+      load_states<kS>(a.A + (int64_t)d * N, n0, N, rate);
+#pragma unroll
+      for (int i = 0; i < kS; ++i) rate[i] = decay_rate(rate[i]);
+    }
+    if constexpr (kStates) {
+      if (span == 0) {   // the initial state into the workspace: the final one may overwrite it
+        float init[kS] = {};
+        if (a.init) load_states<kS>(a.init + state_row, n0, N, init);
+        store_states<kS>(ws_state, n0, N, init);
+      }
+    } else if (p.spans == 1) {
+      if (a.init) load_states<kS>(a.init + state_row, n0, N, h);
+    } else {
+      load_states<kS>(ws_state, n0, N, h);
+      const float* decays = ws_decay + b * p.spans * D + d;
+      constexpr int kAhead = 4;   // spans requested at a time
+      for (int c = 0; c < span; c += kAhead) {
+        float dec[kAhead], end[kAhead][kS];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const int at = c + k < span ? c + k : span - 1;
+          dec[k] = decays[(int64_t)at * D];
+          load_states<kS>(ws_state + (at + 1) * ws_span, n0, N, end[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+          if (c + k < span)
+#pragma unroll
+            for (int i = 0; i < kS; ++i)
+              h[i] = __builtin_fmaf(kTied ? dec[k] : __builtin_amdgcn_exp2f(dec[k] * rate[i]), h[i], end[k][i]);
+      }
+    }
+  }
+
+  // what this thread brings in of a tile: a vector of channels of one token, vectors of B and C.  A last
+  // vector that would pass the group's end (or N) is moved back to end there: the lanes it then shares
+  // with its neighbour in the same wave carry the same values, and channels before the tile are left out.
+  const int st = tid / kVecs;
+  const bool stage = st < kTile;
+  int c0 = tile.first + (tid % kVecs) * kVec;
+  int nc = !stage || c0 >= tile.end ? 0 : kVec;
+  if (nc > 0 && tile.end - c0 < kVec) {
+    if (kFast) c0 = tile.end - kVec;
+    else nc = tile.end - c0;
+  }
+  if (nc == 0) c0 = tile.first;   // for addresses that are not used
+  // dt of a vector: a vector, one head's, several heads'
+  const int mode = kFast ? (kTied ? 1 : 0) : 2;
+  float head_D[kVec], head_bias[kVec], head_rate[kVec];
+#pragma unroll
+  for (int i = 0; i < kVec; ++i) {
+    const int hd = i < nc ? (c0 + i) / P : 0;
+    head_D[i] = a.D && i < nc ? a.D[hd] : 0.0f;
+    head_bias[i] = a.dt_bias && i < nc ? a.dt_bias[hd] : 0.0f;
+    head_rate[i] = kTied && i < nc ? decay_rate(a.A[hd]) : 0.0f;
+  }
+  const int es = dtype == 0 ? 4 : 2, ds = dt_dtype == 0 ? 4 : 2;
+  auto column = [](const void* base, Rows r, int64_t batch, int64_t col, int size) {
+    return static_cast<const char*>(base) + (batch * r.batch + col) * size;
+  };
+  const char* pu = column(a.u, a.ur, b, c0, es);
+  const char* pz = column(a.z, a.zr, b, c0, es);
+  const char* pdt = column(a.dt, a.dtr, b, c0 / P, ds);
+  const char* pB = column(a.B, a.Br, b, (int64_t)group * N, es);
+  const char* pC = column(a.C, a.Cr, b, (int64_t)group * N, es);
+  const int64_t su = a.ur.token * es, sz = a.zr.token * es, sdt = a.dtr.token * ds,
+                sB = a.Br.token * es, sC = a.Cr.token * es;
+  const int64_t t_last = t_end < len ? t_end : len;   // tokens before it are read
+  Raw ru = {}, rz = {}, rdt = {}, rB[kBc], rC[kStates ? 1 : kBc];
+  auto bc_state = [&](int v) {   // first state of vector v of a tile of B, C
+    const int n = (v % (kN / kVec)) * kVec;
+    return kFast && n + kVec > N ? (n < N ? N - kVec : N) : n;
+  };
+  auto fetch = [&](int64_t t0) {
+    const int64_t t = t0 + st;
+    if (t < t_last && nc > 0) {
+      if constexpr (kFast) {
+        request_raw(ru, pu + t * su, dtype);
+        if (!kStates && a.z) request_raw(rz, pz + t * sz, dtype);
+      } else {
+        request_part(ru, pu + t * su, dtype, nc);
+        if (!kStates && a.z) request_part(rz, pz + t * sz, dtype, nc);
+      }
+      const char* row = pdt + t * sdt;
+      if (mode == 0) {
+        request_raw(rdt, row, dt_dtype);
+      } else if (mode == 1) {
+        rdt.w[0] = load_raw1(row, 0, dt_dtype);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (i < nc) rdt.w[i] = load_raw1(row, (c0 + i) / P - c0 / P, dt_dtype);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kBc; ++k) {
+      const int v = tid + k * kThreads, n = bc_state(v);
+      const int64_t tb = t0 + v / (kN / kVec);
+      rB[k] = Raw{};
+      if constexpr (!kStates) rC[k] = Raw{};
+      if (v < kBcVecs && tb < t_last && n < N) {
+        if constexpr (kFast) {
+          request_raw(rB[k], pB + tb * sB + n * es, dtype);
+          if constexpr (!kStates) request_raw(rC[k], pC + tb * sC + n * es, dtype);
+        } else {
+          request_part(rB[k], pB + tb * sB + n * es, dtype, N - n);
+          if constexpr (!kStates) request_part(rC[k], pC + tb * sC + n * es, dtype, N - n);
+        }
+      }
+    }
+  };
+  // what no vector of B, C covers
+  for (int i = tid; i < kTile * kN; i += kThreads) {
+    (&s_B[0][0])[i] = 0.0f;
+    if constexpr (!kStates) (&s_C[0][0])[i] = 0.0f;
+  }
+  __syncthreads();
+
+  float decay = kTied ? 1.0f : 0.0f;   // of the span (kStates)
+  const int lc = c0 - tile.first;   // of this thread's vector in LDS
+  fetch(t_begin);
+  for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
+    float u[kVec], z[kVec];
+    const bool valid = t0 + st < t_last;
+    if (nc > 0) {
+      float dl[kVec], ml[kVec];
+      as_floats(ru, dtype, u);
+      if (!kStates && a.z) as_floats(rz, dtype, z);
+      if (mode == 0) {
+        as_floats(rdt, dt_dtype, dl);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dl[i] = as_float(rdt.w[mode == 1 ? 0 : i], dt_dtype);
+      }
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) {
+        float v = dl[i] + head_bias[i];
+        v = a.dt_softplus ? softplus_fast(v) : v;
+        const bool in = valid && (kFast || i < nc);
+        dl[i] = in ? v : 0.0f;
+        u[i] = in ? u[i] : 0.0f;
+        const float m = kTied ? __builtin_amdgcn_exp2f(dl[i] * head_rate[i]) : dl[i];
+        dl[i] *= u[i];
+        ml[i] = m;
+      }
+      float2* dst = reinterpret_cast<float2*>(&s_du[st][0][0]) + lc;
+      if (kFast && lc >= 0) {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dst[i] = make_float2(ml[i], dl[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kVec; ++i)
+          if (lc + i >= 0 && i < nc) dst[i] = make_float2(ml[i], dl[i]);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kBc; ++k) {
+      const int v = tid + k * kThreads, n = bc_state(v);
+      if ((kBcVecs % kThreads == 0 || v < kBcVecs) && n < N) {
+        const int row = v / (kN / kVec);
+        auto keep = [&](const Raw& r, float* dst) {
+          float f[kVec];
+          as_floats(r, dtype, f);
+          if (kFast && N % 4 == 0) {
+            *reinterpret_cast<float4*>(dst) = make_float4(f[0], f[1], f[2], f[3]);
+            *reinterpret_cast<float4*>(dst + 4) = make_float4(f[4], f[5], f[6], f[7]);
+          } else {
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) dst[i] = f[i];
+          }
+        };
+        keep(rB[k], &s_B[row][n]);
+        if constexpr (!kStates) keep(rC[k], &s_C[row][n]);
+      }
+    }
+    __syncthreads();
+    if (t0 + kTile < t_end) fetch(t0 + kTile);
+    // Tokens in groups of kGroup, the next group's operands on their way from LDS during one's arithmetic
+    // (left to itself the compiler reads each token's right before their use, and a wave alone on its SIMD
+    // waits out the LDS latency three times a token); within a group the exponentials, which depend on
+    // nothing, come first.
+    const int steps = t_end - t0 < kTile ? (int)(t_end - t0 + kPair - 1) / kPair * kPair : kTile;
+    struct Token {
+      float2 du;
+      float B[kS], C[kStates ? 1 : kS];
+    } q[2][kGroup];
+    auto take = [&](int s0, Token (&g)[kGroup]) {
+#pragma unroll
+      for (int j = 0; j < kGroup; ++j) {
+        g[j].du = *reinterpret_cast<const float2*>(&s_du[s0 + j][ch][0]);
+        __builtin_memcpy(g[j].B, __builtin_assume_aligned(&s_B[s0 + j][n0], 16), sizeof(g[j].B));
+        if constexpr (!kStates)
+          __builtin_memcpy(g[j].C, __builtin_assume_aligned(&s_C[s0 + j][n0], 16), sizeof(g[j].C));
+      }
+    };
+    take(0, q[0]);
+    for (int s0 = 0; s0 < steps; s0 += kPair) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int s1 = s0 + half * kGroup;
+        Token(&g)[kGroup] = q[half];
+        take(half == 0 ? s1 + kGroup : (s0 + kPair) % kTile, q[half ^ 1]);
+        __builtin_amdgcn_sched_barrier(0);
+        float m[kGroup][kS], y[kGroup];
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j)
+#pragma unroll
+          for (int i = 0; i < kS; ++i)
+            m[j][i] = kTied ? g[j].du.x : __builtin_amdgcn_exp2f(g[j].du.x * rate[i]);
+#pragma unroll
+        for (int j = 0; j < kGroup; ++j) {
+          y[j] = 0.0f;
+#pragma unroll
+          for (int i = 0; i < kS; ++i) {
+            h[i] = __builtin_fmaf(m[j][i], h[i], g[j].du.y * g[j].B[i]);
+            if constexpr (!kStates) y[j] = __builtin_fmaf(h[i], g[j].C[i], y[j]);
+          }
+          if constexpr (kStates) decay = kTied ? decay * g[j].du.x : decay + g[j].du.x;
+        }
+        if constexpr (!kStates) {
+          lane_sums<kLanes, kGroup>(y);
+          float out = y[0];
+#pragma unroll
+          for (int j = 1; j < kGroup; ++j) out = sub == j ? y[j] : out;
+          if (sub < kGroup) s_du[s1 + sub][ch][0] = out;   // read by this wave alone, and done
+        }
+      }
+    }
+    __syncthreads();
+    if constexpr (!kStates) {
+      if (nc > 0 && t0 + st < t_end) {
+        float y[kVec];
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+          const bool in = (kFast || i < nc) && lc + i >= 0;
+          float v = in ? s_du[st][in ? lc + i : 0][0] : 0.0f;
+          v = __builtin_fmaf(head_D[i], u[i], v);
+          if (a.z) v *= silu(z[i]);
+          y[i] = valid ? v : 0.0f;
+        }
+        const int64_t at = (b * L + t0 + st) * D + c0;
+        if (lc >= 0) {
+          store_as(a.y, at, dtype, kFast ? kVec : nc, y);
+        } else {   // its last nc + lc channels
+          float own[kVec];
+          for (int i = 0; i < kVec; ++i) own[i] = y[i];
+          for (int k = lc; k < 0; ++k)
+#pragma unroll
+            for (int i = 0; i < kVec; ++i) own[i] = i + 1 < kVec ? own[i + 1] : 0.0f;
+          store_as(a.y, at - lc, dtype, kVec + lc, own);
+        }
+      }
+    }
+  }
+  if (!live) return;
+  if constexpr (kStates) {
+    if (sub == 0) ws_decay[(b * p.spans + span) * D + d] = decay;
+    store_states<kS>(ws_state + (span + 1) * ws_span, n0, N, h);
+  } else if (a.final_state && span == p.spans - 1) {
+    store_states<kS>(a.final_state + state_row, n0, N, h);
+  }
+}
+
+// The forms of the kernel with types and layouts fixed at compile time, for the common sizes.
+bool launch_fast(Args& p, hipStream_t st, hipError_t* e);
+
+inline int64_t tiles_of(int64_t channels, int64_t groups, int64_t per) {
+  return groups * ((channels / groups + per - 1) / per);
+}
+
+template <int kLanes, int kS, bool kTied, int kType, int kDt, bool kFast>
+hipError_t launch_form(Args& p, hipStream_t st) {
+  p.group_tiles = (int)tiles_of(p.group_ch, 1, kThreads / kLanes);
+  const int64_t tiles = p.s.batch * p.s.ngroups * p.group_tiles;
+  if (p.spans > 1) {
+    scan_kernel<kLanes, kS, kTied, true, kType, kDt, kFast>
+        <<<dim3((unsigned)(tiles * (p.spans - 1))), kThreads, 0, st>>>(p);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  scan_kernel<kLanes, kS, kTied, false, kType, kDt, kFast>
+      <<<dim3((unsigned)(tiles * p.spans)), kThreads, 0, st>>>(p);
+  return hipGetLastError();
+}
+
+}  // namespace sel_scan
+}  // namespace ssdi8
