@@ -89,6 +89,17 @@ __device__ __forceinline__ void store_states(float* row, int n0, int N, const fl
   }
 }
 
+// Where channel pair `pair` of a token's row of kVecs * 4 pairs lies: the low two bits of its place are
+// exchanged so that the 16 lanes of an access, neighbouring vectors and tokens, touch every bank once.
+template <int kVecs> __device__ __forceinline__ int pair_slot(int row, int pair) {
+  int key;
+  if (kVecs == 8) key = (pair >> 4) ^ ((row & 1) << 1);
+  else if (kVecs == 4) key = row & 3;
+  else if (kVecs == 2) key = (row >> 1) & 3;
+  else key = (row >> 2) & 3;
+  return pair ^ key;
+}
+
 struct Args {
   SelScan s;
   int64_t span;          // tokens of a span (a multiple of kTile)
@@ -123,7 +134,11 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   constexpr int kBcVecs = kTile * (kN / kVec);      // vectors of a tile of B (or C)
   constexpr int kBc = (kBcVecs + kThreads - 1) / kThreads;
   static_assert(kCh % kVec == 0 && kVecs * kTile <= kThreads && kN % kVec == 0, "tile");
-  __shared__ __attribute__((aligned(16))) float s_du[kTile][kCh][2];   // delta (or decay), delta u
+  // delta (or decay) and delta u of a tile, pairs of channels (16 bytes) exchanged by pair_slot; the sums
+  // of y, rows apart by a quarter of the banks
+  __shared__ __attribute__((aligned(16))) float s_du[kTile][kCh * 2];
+  constexpr int kYRow = kCh + 16;
+  __shared__ __attribute__((aligned(16))) float s_y[kStates ? 1 : kTile][kStates ? 4 : kYRow];
   __shared__ __attribute__((aligned(16))) float s_B[kTile][kN];
   __shared__ __attribute__((aligned(16))) float s_C[kStates ? 1 : kTile][kStates ? 4 : kN];
 
@@ -275,12 +290,33 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   }
   __syncthreads();
 
-  float decay = kTied ? 1.0f : 0.0f;   // of the span (kStates)
   const int lc = c0 - tile.first;   // of this thread's vector in LDS
+  // A tile's y is stored behind the next tile's loads: loads and stores count down in one order, and the
+  // wait for the loads, had it the store before it, would be for that too.
+  float done[kVec] = {};
+  auto put_y = [&](int64_t t0) {
+    if (nc == 0 || t0 < t_begin || t0 + st >= t_end) return;
+    const int64_t at = (b * L + t0 + st) * D + c0;
+    if (lc >= 0) {
+      store_as(a.y, at, dtype, kFast ? kVec : nc, done);
+    } else {   // a vector moved back from the group's end: its last kVec + lc channels
+      float own[kVec];
+#pragma unroll
+      for (int i = 0; i < kVec; ++i) own[i] = done[i];
+      for (int k = lc; k < 0; ++k)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) own[i] = i + 1 < kVec ? own[i + 1] : 0.0f;
+      store_as(a.y, at - lc, dtype, kVec + lc, own);
+    }
+  };
+  float decay = kTied ? 1.0f : 0.0f;   // of the span (kStates)
   fetch(t_begin);
   for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
     float u[kVec], z[kVec];
     const bool valid = t0 + st < t_last;
+    // every load of this tile; said here, where every lane comes by, it spares the waits that the compiler
+    // puts before the next requests on behalf of lanes that skip what follows
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
     if (nc > 0) {
       float dl[kVec], ml[kVec];
       as_floats(ru, dtype, u);
@@ -292,24 +328,32 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
         for (int i = 0; i < kVec; ++i) dl[i] = as_float(rdt.w[mode == 1 ? 0 : i], dt_dtype);
       }
 #pragma unroll
+      for (int i = 0; i < kVec; ++i) dl[i] += head_bias[i];
+      if (a.dt_softplus)
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) dl[i] = softplus_fast(dl[i]);
+#pragma unroll
       for (int i = 0; i < kVec; ++i) {
-        float v = dl[i] + head_bias[i];
-        v = a.dt_softplus ? softplus_fast(v) : v;
         const bool in = valid && (kFast || i < nc);
-        dl[i] = in ? v : 0.0f;
+        dl[i] = in ? dl[i] : 0.0f;
         u[i] = in ? u[i] : 0.0f;
         const float m = kTied ? __builtin_amdgcn_exp2f(dl[i] * head_rate[i]) : dl[i];
         dl[i] *= u[i];
         ml[i] = m;
       }
-      float2* dst = reinterpret_cast<float2*>(&s_du[st][0][0]) + lc;
-      if (kFast && lc >= 0) {
+      if (kFast && lc % kVec == 0) {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) dst[i] = make_float2(ml[i], dl[i]);
+        for (int i = 0; i < kVec; i += 2)
+          *reinterpret_cast<float4*>(&s_du[st][4 * pair_slot<kVecs>(st, (lc + i) / 2)]) =
+              make_float4(ml[i], dl[i], ml[i + 1], dl[i + 1]);
       } else {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
-          if (lc + i >= 0 && i < nc) dst[i] = make_float2(ml[i], dl[i]);
+        for (int i = 0; i < kVec; ++i) {
+          const int c = lc + i;
+          if (c >= 0 && (kFast || i < nc))
+            *reinterpret_cast<float2*>(&s_du[st][4 * pair_slot<kVecs>(st, c / 2) + 2 * (c & 1)]) =
+                make_float2(ml[i], dl[i]);
+        }
       }
     }
 #pragma unroll
@@ -320,7 +364,7 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
         auto keep = [&](const Raw& r, float* dst) {
           float f[kVec];
           as_floats(r, dtype, f);
-          if (kFast && N % 4 == 0) {
+          if constexpr (kFast) {
             *reinterpret_cast<float4*>(dst) = make_float4(f[0], f[1], f[2], f[3]);
             *reinterpret_cast<float4*>(dst + 4) = make_float4(f[4], f[5], f[6], f[7]);
           } else {
@@ -332,6 +376,7 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
         if constexpr (!kStates) keep(rC[k], &s_C[row][n]);
       }
     }
+    if constexpr (!kStates) put_y(t0 - kTile);
     __syncthreads();
     if (t0 + kTile < t_end) fetch(t0 + kTile);
     // Tokens in groups of kGroup, the next group's operands on their way from LDS during one's arithmetic
@@ -346,7 +391,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
     auto take = [&](int s0, Token (&g)[kGroup]) {
 #pragma unroll
       for (int j = 0; j < kGroup; ++j) {
-        g[j].du = *reinterpret_cast<const float2*>(&s_du[s0 + j][ch][0]);
+        g[j].du = *reinterpret_cast<const float2*>(
+            &s_du[s0 + j][4 * pair_slot<kVecs>(s0 + j, ch / 2) + 2 * (ch & 1)]);
         __builtin_memcpy(g[j].B, __builtin_assume_aligned(&s_B[s0 + j][n0], 16), sizeof(g[j].B));
         if constexpr (!kStates)
           __builtin_memcpy(g[j].C, __builtin_assume_aligned(&s_C[s0 + j][n0], 16), sizeof(g[j].C));
@@ -381,36 +427,34 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
           float out = y[0];
 #pragma unroll
           for (int j = 1; j < kGroup; ++j) out = sub == j ? y[j] : out;
-          if (sub < kGroup) s_du[s1 + sub][ch][0] = out;   // read by this wave alone, and done
+          if (sub < kGroup) s_y[s1 + sub][ch] = out;
         }
       }
     }
     __syncthreads();
     if constexpr (!kStates) {
       if (nc > 0 && t0 + st < t_end) {
-        float y[kVec];
+        float sum[kVec];
+        if (kFast && lc % kVec == 0) {
+          __builtin_memcpy(sum, __builtin_assume_aligned(&s_y[st][lc], 16), sizeof(sum));
+        } else {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-          const bool in = (kFast || i < nc) && lc + i >= 0;
-          float v = in ? s_du[st][in ? lc + i : 0][0] : 0.0f;
-          v = __builtin_fmaf(head_D[i], u[i], v);
-          if (a.z) v *= silu(z[i]);
-          y[i] = valid ? v : 0.0f;
+          for (int i = 0; i < kVec; ++i) {
+            const bool in = lc + i >= 0 && (kFast || i < nc);
+            sum[i] = in ? s_y[st][in ? lc + i : 0] : 0.0f;
+          }
         }
-        const int64_t at = (b * L + t0 + st) * D + c0;
-        if (lc >= 0) {
-          store_as(a.y, at, dtype, kFast ? kVec : nc, y);
-        } else {   // its last nc + lc channels
-          float own[kVec];
-          for (int i = 0; i < kVec; ++i) own[i] = y[i];
-          for (int k = lc; k < 0; ++k)
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) own[i] = i + 1 < kVec ? own[i + 1] : 0.0f;
-          store_as(a.y, at - lc, dtype, kVec + lc, own);
-        }
+        for (int i = 0; i < kVec; ++i) done[i] = __builtin_fmaf(head_D[i], u[i], sum[i]);
+        if (a.z)
+#pragma unroll
+          for (int i = 0; i < kVec; ++i) done[i] *= silu(z[i]);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) done[i] = valid ? done[i] : 0.0f;
       }
     }
   }
+  if constexpr (!kStates) put_y(t_begin + (t_end - t_begin - 1) / kTile * kTile);
   if (!live) return;
   if constexpr (kStates) {
     if (sub == 0) ws_decay[(b * p.spans + span) * D + d] = decay;

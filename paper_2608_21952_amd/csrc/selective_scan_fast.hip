@@ -21,7 +21,7 @@ template <int kLanes, int kS, bool kTied> hipError_t by_type(Args& p, hipStream_
 
 bool launch_fast(Args& p, hipStream_t st, hipError_t* e) {
   const SelScan& a = p.s;
-  if (p.group_ch < kVec || a.dstate < kVec) return false;
+  if (p.group_ch < kVec || a.dstate < kVec || a.dstate % 4 != 0) return false;
   if (a.tied) {
     if (a.headdim % kVec != 0 || p.group_ch % kVec != 0 || a.dstate <= 32 || a.dstate > 128) return false;
     *e = a.dstate <= 64 ? by_type<16, 4, true>(p, st) : by_type<16, 8, true>(p, st);
