@@ -29,13 +29,13 @@ using namespace sel_scan;
 
 template <typename F> hipError_t for_states(int64_t N, F&& f) {
   using std::integral_constant;
-  if (N <= 16) return f(integral_constant<int, 4>(), integral_constant<int, 4>());
+  if (N <= 16) return f(integral_constant<int, 8>(), integral_constant<int, 2>());
   if (N <= 32) return f(integral_constant<int, 8>(), integral_constant<int, 4>());
   if (N <= 64) return f(integral_constant<int, 16>(), integral_constant<int, 4>());
   if (N <= 128) return f(integral_constant<int, 16>(), integral_constant<int, 8>());
   return f(integral_constant<int, 32>(), integral_constant<int, 8>());
 }
-int lanes_of(int64_t N) { return N <= 16 ? 4 : N <= 32 ? 8 : N <= 128 ? 16 : 32; }
+int lanes_of(int64_t N) { return N <= 32 ? 8 : N <= 128 ? 16 : 32; }
 
 // ---------------------------------------------------------------------------- one token
 // kLanes lanes hold a channel, four states each: neighbouring ones (kWide: one 16-byte access, N a
@@ -123,9 +123,12 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(Args p, float* stat
 
 int sel_scan_spans(int64_t batch, int64_t seqlen, int64_t channels, int64_t groups, int64_t dstate) {
   const int64_t wgs = batch * tiles_of(channels, groups, kThreads / lanes_of(dstate));
+  // Uncut from a workgroup per CU on: a cut costs the walk a second time, less what only y needs (8 x 2048 x
+  // 1536 x 16, 384 workgroups: 191 us uncut, 217 in 2 spans; 4 x 4096 x 5120, 640: 566 and 632).  Below, three
+  // workgroups per CU (1 x 16384 x 1536, 48: 905 us uncut, 232 in 16 spans, 230 in 32), of 128 tokens or more.
   if (wgs >= 256 || wgs == 0) return 1;
   const int64_t most = (seqlen + 127) / 128;
-  int64_t spans = 1024 / wgs;
+  int64_t spans = 768 / wgs;
   if (spans > most) spans = most;
   return spans < 2 ? 1 : (int)spans;
 }
@@ -143,7 +146,7 @@ hipError_t launch_sel_scan(const SelScan& a, hipStream_t st) {
   p.group_ch = p.D / (int)a.ngroups;
   p.spans = sel_scan_spans(a.batch, a.seqlen, p.D, a.ngroups, a.dstate);
   const int64_t tokens = (a.seqlen + p.spans - 1) / p.spans;
-  p.span = (tokens + kTile - 1) / kTile * kTile;
+  p.span = (tokens + kSpanTokens - 1) / kSpanTokens * kSpanTokens;
   // rounding up may leave spans without tokens: fewer are launched
   if (p.span > 0) p.spans = (int)((a.seqlen + p.span - 1) / p.span);
   if (p.spans < 1) p.spans = 1;
@@ -151,8 +154,8 @@ hipError_t launch_sel_scan(const SelScan& a, hipStream_t st) {
   if (launch_fast(p, st, &e)) return e;
   return for_states(a.dstate, [&](auto lanes, auto states) {
     constexpr int kLanes = decltype(lanes)::value, kS = decltype(states)::value;
-    return a.tied ? launch_form<kLanes, kS, true, -1, -1, false>(p, st)
-                  : launch_form<kLanes, kS, false, -1, -1, false>(p, st);
+    return a.tied ? launch_form<kLanes, kS, 32, 8, true, -1, -1, false>(p, st)
+                  : launch_form<kLanes, kS, 32, 8, false, -1, -1, false>(p, st);
   });
 }
 

@@ -9,25 +9,27 @@ namespace ssdi8 {
 
 namespace sel_scan {
 
-constexpr int kTile = 32;
 constexpr int kThreads = 256;
+constexpr int kSpanTokens = 64;   // the longest tile
 
-// kVec elements as they lie in memory (8 words of fp32, 4 of a 16-bit type), turned into fp32 later.  A
-// whole vector is requested without a choice between ways of loading it: where ways met, the compiler
-// waited for the data.
-struct Raw {
-  uint32_t w[kVec];
+// kCount elements as they lie in memory (a word each of fp32, half a word of a 16-bit type), turned into
+// fp32 later.  A whole vector is requested without a choice between ways of loading it: where ways met, the
+// compiler waited for the data.
+template <int kCount> struct Raw {
+  uint32_t w[kCount];
 };
-__device__ __forceinline__ void request_raw(Raw& r, const char* p, int dtype) {
-  __builtin_memcpy(r.w, p, 16);
-  if (dtype == 0) __builtin_memcpy(r.w + 4, p + 16, 16);
+template <int kCount>
+__device__ __forceinline__ void request_raw(Raw<kCount>& r, const char* p, int dtype) {
+  __builtin_memcpy(r.w, p, 2 * kCount);
+  if (dtype == 0) __builtin_memcpy(r.w + kCount / 2, p + 2 * kCount, 2 * kCount);
 }
 // The first n elements, the others 0.
-__device__ __forceinline__ void request_part(Raw& r, const char* p, int dtype, int n) {
+template <int kCount>
+__device__ __forceinline__ void request_part(Raw<kCount>& r, const char* p, int dtype, int n) {
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) r.w[i] = 0;
+  for (int i = 0; i < kCount; ++i) r.w[i] = 0;
 #pragma unroll
-  for (int i = 0; i < kVec; ++i)
+  for (int i = 0; i < kCount; ++i)
     if (i < n) {
       if (dtype == 0) r.w[i] = reinterpret_cast<const uint32_t*>(p)[i];
       else r.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
@@ -42,25 +44,39 @@ __device__ __forceinline__ float as_float(uint32_t bits, int dtype) {
   if (dtype == 1) return (float)__builtin_bit_cast(_Float16, (uint16_t)bits);
   return __builtin_bit_cast(float, bits << 16);
 }
-__device__ __forceinline__ void as_floats(const Raw& r, int dtype, float (&out)[kVec]) {
+template <int kCount>
+__device__ __forceinline__ void as_floats(const Raw<kCount>& r, int dtype, float (&out)[kCount]) {
   if (dtype == 0) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i) out[i] = __builtin_bit_cast(float, r.w[i]);
+    for (int i = 0; i < kCount; ++i) out[i] = __builtin_bit_cast(float, r.w[i]);
   } else if (dtype == 1) {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i)
+    for (int i = 0; i < kCount; ++i)
       out[i] = (float)__builtin_bit_cast(_Float16, (uint16_t)(r.w[i / 2] >> (16 * (i & 1))));
   } else {
 #pragma unroll
-    for (int i = 0; i < kVec; ++i)
+    for (int i = 0; i < kCount; ++i)
       out[i] = __builtin_bit_cast(float, i & 1 ? r.w[i / 2] & 0xffff0000u : r.w[i / 2] << 16);
   }
 }
-__device__ __forceinline__ void store_as(void* base, int64_t off, int dtype, int n,
-                                         const float (&v)[kVec]) {
-  if (dtype == 0) store_vec<float>(static_cast<float*>(base) + off, n, v);
-  else if (dtype == 1) store_vec<_Float16>(static_cast<_Float16*>(base) + off, n, v);
-  else store_vec<bf16>(static_cast<bf16*>(base) + off, n, v);
+template <typename T, int kCount>
+__device__ __forceinline__ void store_n(T* p, int n, const float (&v)[kCount]) {
+  if (n >= kCount) {
+    T t[kCount];
+#pragma unroll
+    for (int i = 0; i < kCount; ++i) t[i] = (T)v[i];
+    __builtin_memcpy(p, t, sizeof(t));
+  } else {
+#pragma unroll
+    for (int i = 0; i < kCount; ++i)
+      if (i < n) p[i] = (T)v[i];
+  }
+}
+template <int kCount>
+__device__ __forceinline__ void store_as(void* base, int64_t off, int dtype, int n, const float (&v)[kCount]) {
+  if (dtype == 0) store_n(static_cast<float*>(base) + off, n, v);
+  else if (dtype == 1) store_n(static_cast<_Float16*>(base) + off, n, v);
+  else store_n(static_cast<bf16*>(base) + off, n, v);
 }
 
 // A in base 2; -inf (a decay of 0 for any positive delta) stays finite, so that delta = 0 gives 1.
@@ -89,20 +105,71 @@ __device__ __forceinline__ void store_states(float* row, int n0, int N, const fl
   }
 }
 
-// Where channel pair `pair` of a token's row of kVecs * 4 pairs lies: the low two bits of its place are
-// exchanged so that the 16 lanes of an access, neighbouring vectors and tokens, touch every bank once.
-template <int kVecs> __device__ __forceinline__ int pair_slot(int row, int pair) {
+// Where channel pair `pair` of a token's row of kCh channels lies.  With vectors of eight channels the low two
+// bits of its place are exchanged so that the 16 lanes of an access, neighbouring vectors and tokens, touch
+// every bank once; pairs by themselves lie in a line.
+template <int kCh, int kSV> __device__ __forceinline__ int pair_slot(int row, int pair) {
+  if (kSV != 8) return pair;
   int key;
-  if (kVecs == 8) key = (pair >> 4) ^ ((row & 1) << 1);
-  else if (kVecs == 4) key = row & 3;
-  else if (kVecs == 2) key = (row >> 1) & 3;
+  if (kCh == 64) key = (pair >> 4) ^ ((row & 1) << 1);
+  else if (kCh == 32) key = row & 3;
+  else if (kCh == 16) key = (row >> 1) & 3;
   else key = (row >> 2) & 3;
   return pair ^ key;
 }
 
+// The sums over kLanes lanes of kGroup tokens' values, each token's in lanes of its own: while more than one
+// value is left, a lane keeps those of one half of the tokens and gives its partner the others, so that a
+// step costs half of the one before it.  Partners in order: 16 lanes off, mirrored in 16 and in 8 (they
+// differ in the bit that chooses, and hold the same tokens), then neighbours and pairs.
+constexpr int kSumBits[5] = {4, 3, 2, 0, 1};
+template <int kStep> __device__ __forceinline__ float partner(float v) {
+  constexpr int kCtrl = kStep == 1 ? 0x140 : kStep == 2 ? 0x141 : kStep == 3 ? 0xB1 : 0x4E;
+  if constexpr (kStep == 0) return __shfl_xor(v, 16);
+  else
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), kCtrl, 0xf,
+                                                                 0xf, true));
+}
+constexpr int sum_first(int lanes) {   // the first of the steps
+  return lanes == 32 ? 0 : lanes == 16 ? 1 : lanes == 8 ? 2 : 3;
+}
+template <int kStep, int kCount>
+__device__ __forceinline__ float sum_steps(const float (&v)[kCount], int lane) {
+  if constexpr (kStep == 5) {
+    return v[0];
+  } else if constexpr (kCount == 1) {
+    const float s[1] = {v[0] + partner<kStep>(v[0])};
+    return sum_steps<kStep + 1, 1>(s, lane);
+  } else {
+    const bool odd = (lane >> kSumBits[kStep]) & 1;
+    float s[kCount / 2];
+#pragma unroll
+    for (int i = 0; i < kCount / 2; ++i)
+      s[i] = (odd ? v[2 * i + 1] : v[2 * i]) + partner<kStep>(odd ? v[2 * i] : v[2 * i + 1]);
+    return sum_steps<kStep + 1, kCount / 2>(s, lane);
+  }
+}
+template <int kLanes, int kGroup>
+__device__ __forceinline__ float sum_tokens(const float (&v)[kGroup], int lane) {
+  return sum_steps<sum_first(kLanes), kGroup>(v, lane);
+}
+// The token whose sum a lane ends up with, and whether it is the one lane that stores it.
+template <int kLanes, int kGroup> __device__ __forceinline__ int token_of(int lane) {
+  int t = 0, step = sum_first(kLanes);
+#pragma unroll
+  for (int k = 0; (1 << k) < kGroup; ++k) t |= ((lane >> kSumBits[step++]) & 1) << k;
+  return t;
+}
+template <int kLanes, int kGroup> __device__ __forceinline__ bool writes_token(int lane) {
+  int step = sum_first(kLanes);
+#pragma unroll
+  for (int k = 0; (1 << k) < kGroup; ++k) lane &= ~(1 << kSumBits[step++]);
+  return lane == 0;
+}
+
 struct Args {
   SelScan s;
-  int64_t span;          // tokens of a span (a multiple of kTile)
+  int64_t span;          // tokens of a span (a multiple of kSpanTokens)
   int spans, D;
   int group_ch, group_tiles;   // channels of a group, workgroups that hold them
 };
@@ -125,15 +192,16 @@ __device__ __forceinline__ Tile tile_of(const Args& p, int ct, int channels) {
 // takes everything, element by element where it has to, and waits for its loads.
 // Workspace of a cut scan: states [b, spans, d, n] (0: the initial state, c + 1: span c's from zero),
 // then the spans' decays [b, spans, d].
-template <int kLanes, int kS, bool kTied, bool kStates, int kType, int kDt, bool kFast>
+// kTile: tokens of a tile.  kSV: channels of a thread's part of a tile, so that all threads have one.
+template <int kLanes, int kS, int kTile, int kSV, bool kTied, bool kStates, int kType, int kDt, bool kFast>
 __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   constexpr int kCh = kThreads / kLanes;            // channels of a workgroup
   constexpr int kN = kLanes * kS;                   // states, padded
-  constexpr int kGroup = kS > 4 ? 2 : 4, kPair = 2 * kGroup;
-  constexpr int kVecs = kCh / kVec;                 // vectors of a token's channels
+  constexpr int kGroup = kS > 4 ? 2 : kS == 4 ? 4 : 8, kPair = 2 * kGroup;
+  constexpr int kVecs = kCh / kSV;                  // vectors of a token's channels
   constexpr int kBcVecs = kTile * (kN / kVec);      // vectors of a tile of B (or C)
   constexpr int kBc = (kBcVecs + kThreads - 1) / kThreads;
-  static_assert(kCh % kVec == 0 && kVecs * kTile <= kThreads && kN % kVec == 0, "tile");
+  static_assert(kCh % kSV == 0 && 64 % kVecs == 0 && kVecs * kTile <= kThreads && kN % kVec == 0, "tile");
   // delta (or decay) and delta u of a tile, pairs of channels (16 bytes) exchanged by pair_slot; the sums
   // of y, rows apart by a quarter of the banks
   __shared__ __attribute__((aligned(16))) float s_du[kTile][kCh * 2];
@@ -211,18 +279,18 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   // with its neighbour in the same wave carry the same values, and channels before the tile are left out.
   const int st = tid / kVecs;
   const bool stage = st < kTile;
-  int c0 = tile.first + (tid % kVecs) * kVec;
-  int nc = !stage || c0 >= tile.end ? 0 : kVec;
-  if (nc > 0 && tile.end - c0 < kVec) {
-    if (kFast) c0 = tile.end - kVec;
+  int c0 = tile.first + (tid % kVecs) * kSV;
+  int nc = !stage || c0 >= tile.end ? 0 : kSV;
+  if (nc > 0 && tile.end - c0 < kSV) {
+    if (kFast) c0 = tile.end - kSV;
     else nc = tile.end - c0;
   }
   if (nc == 0) c0 = tile.first;   // for addresses that are not used
   // dt of a vector: a vector, one head's, several heads'
   const int mode = kFast ? (kTied ? 1 : 0) : 2;
-  float head_D[kVec], head_bias[kVec], head_rate[kVec];
+  float head_D[kSV], head_bias[kSV], head_rate[kSV];
 #pragma unroll
-  for (int i = 0; i < kVec; ++i) {
+  for (int i = 0; i < kSV; ++i) {
     const int hd = i < nc ? (c0 + i) / P : 0;
     head_D[i] = a.D && i < nc ? a.D[hd] : 0.0f;
     head_bias[i] = a.dt_bias && i < nc ? a.dt_bias[hd] : 0.0f;
@@ -240,7 +308,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   const int64_t su = a.ur.token * es, sz = a.zr.token * es, sdt = a.dtr.token * ds,
                 sB = a.Br.token * es, sC = a.Cr.token * es;
   const int64_t t_last = t_end < len ? t_end : len;   // tokens before it are read
-  Raw ru = {}, rz = {}, rdt = {}, rB[kBc], rC[kStates ? 1 : kBc];
+  Raw<kSV> ru = {}, rz = {}, rdt = {};
+  Raw<kVec> rB[kBc], rC[kStates ? 1 : kBc];
   auto bc_state = [&](int v) {   // first state of vector v of a tile of B, C
     const int n = (v % (kN / kVec)) * kVec;
     return kFast && n + kVec > N ? (n < N ? N - kVec : N) : n;
@@ -262,7 +331,7 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
         rdt.w[0] = load_raw1(row, 0, dt_dtype);
       } else {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i)
+        for (int i = 0; i < kSV; ++i)
           if (i < nc) rdt.w[i] = load_raw1(row, (c0 + i) / P - c0 / P, dt_dtype);
       }
     }
@@ -270,8 +339,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
     for (int k = 0; k < kBc; ++k) {
       const int v = tid + k * kThreads, n = bc_state(v);
       const int64_t tb = t0 + v / (kN / kVec);
-      rB[k] = Raw{};
-      if constexpr (!kStates) rC[k] = Raw{};
+      rB[k] = {};
+      if constexpr (!kStates) rC[k] = {};
       if (v < kBcVecs && tb < t_last && n < N) {
         if constexpr (kFast) {
           request_raw(rB[k], pB + tb * sB + n * es, dtype);
@@ -283,6 +352,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
       }
     }
   };
+  const int y_token = token_of<kLanes, kGroup>(sub);
+  const bool y_writer = writes_token<kLanes, kGroup>(sub);
   // what no vector of B, C covers
   for (int i = tid; i < kTile * kN; i += kThreads) {
     (&s_B[0][0])[i] = 0.0f;
@@ -293,47 +364,47 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   const int lc = c0 - tile.first;   // of this thread's vector in LDS
   // A tile's y is stored behind the next tile's loads: loads and stores count down in one order, and the
   // wait for the loads, had it the store before it, would be for that too.
-  float done[kVec] = {};
+  float done[kSV] = {};
   auto put_y = [&](int64_t t0) {
     if (nc == 0 || t0 < t_begin || t0 + st >= t_end) return;
     const int64_t at = (b * L + t0 + st) * D + c0;
     if (lc >= 0) {
-      store_as(a.y, at, dtype, kFast ? kVec : nc, done);
-    } else {   // a vector moved back from the group's end: its last kVec + lc channels
-      float own[kVec];
+      store_as(a.y, at, dtype, kFast ? kSV : nc, done);
+    } else {   // a vector moved back from the group's end: its last kSV + lc channels
+      float own[kSV];
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) own[i] = done[i];
+      for (int i = 0; i < kSV; ++i) own[i] = done[i];
       for (int k = lc; k < 0; ++k)
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) own[i] = i + 1 < kVec ? own[i + 1] : 0.0f;
-      store_as(a.y, at - lc, dtype, kVec + lc, own);
+        for (int i = 0; i < kSV; ++i) own[i] = i + 1 < kSV ? own[i + 1] : 0.0f;
+      store_as(a.y, at - lc, dtype, kSV + lc, own);
     }
   };
   float decay = kTied ? 1.0f : 0.0f;   // of the span (kStates)
   fetch(t_begin);
   for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
-    float u[kVec], z[kVec];
+    float u[kSV], z[kSV];
     const bool valid = t0 + st < t_last;
     // every load of this tile; said here, where every lane comes by, it spares the waits that the compiler
     // puts before the next requests on behalf of lanes that skip what follows
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
     if (nc > 0) {
-      float dl[kVec], ml[kVec];
+      float dl[kSV], ml[kSV];
       as_floats(ru, dtype, u);
       if (!kStates && a.z) as_floats(rz, dtype, z);
       if (mode == 0) {
         as_floats(rdt, dt_dtype, dl);
       } else {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) dl[i] = as_float(rdt.w[mode == 1 ? 0 : i], dt_dtype);
+        for (int i = 0; i < kSV; ++i) dl[i] = as_float(rdt.w[mode == 1 ? 0 : i], dt_dtype);
       }
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) dl[i] += head_bias[i];
+      for (int i = 0; i < kSV; ++i) dl[i] += head_bias[i];
       if (a.dt_softplus)
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) dl[i] = softplus_fast(dl[i]);
+        for (int i = 0; i < kSV; ++i) dl[i] = softplus_fast(dl[i]);
 #pragma unroll
-      for (int i = 0; i < kVec; ++i) {
+      for (int i = 0; i < kSV; ++i) {
         const bool in = valid && (kFast || i < nc);
         dl[i] = in ? dl[i] : 0.0f;
         u[i] = in ? u[i] : 0.0f;
@@ -341,17 +412,17 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
         dl[i] *= u[i];
         ml[i] = m;
       }
-      if (kFast && lc % kVec == 0) {
+      if (kFast && lc % kSV == 0) {
 #pragma unroll
-        for (int i = 0; i < kVec; i += 2)
-          *reinterpret_cast<float4*>(&s_du[st][4 * pair_slot<kVecs>(st, (lc + i) / 2)]) =
+        for (int i = 0; i < kSV; i += 2)
+          *reinterpret_cast<float4*>(&s_du[st][4 * pair_slot<kCh, kSV>(st, (lc + i) / 2)]) =
               make_float4(ml[i], dl[i], ml[i + 1], dl[i + 1]);
       } else {
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) {
+        for (int i = 0; i < kSV; ++i) {
           const int c = lc + i;
           if (c >= 0 && (kFast || i < nc))
-            *reinterpret_cast<float2*>(&s_du[st][4 * pair_slot<kVecs>(st, c / 2) + 2 * (c & 1)]) =
+            *reinterpret_cast<float2*>(&s_du[st][4 * pair_slot<kCh, kSV>(st, c / 2) + 2 * (c & 1)]) =
                 make_float2(ml[i], dl[i]);
         }
       }
@@ -361,7 +432,7 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
       const int v = tid + k * kThreads, n = bc_state(v);
       if ((kBcVecs % kThreads == 0 || v < kBcVecs) && n < N) {
         const int row = v / (kN / kVec);
-        auto keep = [&](const Raw& r, float* dst) {
+        auto keep = [&](const Raw<kVec>& r, float* dst) {
           float f[kVec];
           as_floats(r, dtype, f);
           if constexpr (kFast) {
@@ -392,10 +463,10 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
 #pragma unroll
       for (int j = 0; j < kGroup; ++j) {
         g[j].du = *reinterpret_cast<const float2*>(
-            &s_du[s0 + j][4 * pair_slot<kVecs>(s0 + j, ch / 2) + 2 * (ch & 1)]);
-        __builtin_memcpy(g[j].B, __builtin_assume_aligned(&s_B[s0 + j][n0], 16), sizeof(g[j].B));
+            &s_du[s0 + j][4 * pair_slot<kCh, kSV>(s0 + j, ch / 2) + 2 * (ch & 1)]);
+        __builtin_memcpy(g[j].B, __builtin_assume_aligned(&s_B[s0 + j][n0], kS > 2 ? 16 : 8), sizeof(g[j].B));
         if constexpr (!kStates)
-          __builtin_memcpy(g[j].C, __builtin_assume_aligned(&s_C[s0 + j][n0], 16), sizeof(g[j].C));
+          __builtin_memcpy(g[j].C, __builtin_assume_aligned(&s_C[s0 + j][n0], kS > 2 ? 16 : 8), sizeof(g[j].C));
       }
     };
     take(0, q[0]);
@@ -423,34 +494,31 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
           if constexpr (kStates) decay = kTied ? decay * g[j].du.x : decay + g[j].du.x;
         }
         if constexpr (!kStates) {
-          lane_sums<kLanes, kGroup>(y);
-          float out = y[0];
-#pragma unroll
-          for (int j = 1; j < kGroup; ++j) out = sub == j ? y[j] : out;
-          if (sub < kGroup) s_y[s1 + sub][ch] = out;
+          const float sum = sum_tokens<kLanes, kGroup>(y, sub);
+          if (y_writer) s_y[s1 + y_token][ch] = sum;
         }
       }
     }
     __syncthreads();
     if constexpr (!kStates) {
       if (nc > 0 && t0 + st < t_end) {
-        float sum[kVec];
-        if (kFast && lc % kVec == 0) {
-          __builtin_memcpy(sum, __builtin_assume_aligned(&s_y[st][lc], 16), sizeof(sum));
+        float sum[kSV];
+        if (kFast && lc % kSV == 0) {
+          __builtin_memcpy(sum, __builtin_assume_aligned(&s_y[st][lc], kSV > 2 ? 16 : 8), sizeof(sum));
         } else {
 #pragma unroll
-          for (int i = 0; i < kVec; ++i) {
+          for (int i = 0; i < kSV; ++i) {
             const bool in = lc + i >= 0 && (kFast || i < nc);
             sum[i] = in ? s_y[st][in ? lc + i : 0] : 0.0f;
           }
         }
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) done[i] = __builtin_fmaf(head_D[i], u[i], sum[i]);
+        for (int i = 0; i < kSV; ++i) done[i] = __builtin_fmaf(head_D[i], u[i], sum[i]);
         if (a.z)
 #pragma unroll
-          for (int i = 0; i < kVec; ++i) done[i] *= silu(z[i]);
+          for (int i = 0; i < kSV; ++i) done[i] *= silu(z[i]);
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) done[i] = valid ? done[i] : 0.0f;
+        for (int i = 0; i < kSV; ++i) done[i] = valid ? done[i] : 0.0f;
       }
     }
   }
@@ -471,17 +539,17 @@ inline int64_t tiles_of(int64_t channels, int64_t groups, int64_t per) {
   return groups * ((channels / groups + per - 1) / per);
 }
 
-template <int kLanes, int kS, bool kTied, int kType, int kDt, bool kFast>
+template <int kLanes, int kS, int kTile, int kSV, bool kTied, int kType, int kDt, bool kFast>
 hipError_t launch_form(Args& p, hipStream_t st) {
   p.group_tiles = (int)tiles_of(p.group_ch, 1, kThreads / kLanes);
   const int64_t tiles = p.s.batch * p.s.ngroups * p.group_tiles;
   if (p.spans > 1) {
-    scan_kernel<kLanes, kS, kTied, true, kType, kDt, kFast>
+    scan_kernel<kLanes, kS, kTile, kSV, kTied, true, kType, kDt, kFast>
         <<<dim3((unsigned)(tiles * (p.spans - 1))), kThreads, 0, st>>>(p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  scan_kernel<kLanes, kS, kTied, false, kType, kDt, kFast>
+  scan_kernel<kLanes, kS, kTile, kSV, kTied, false, kType, kDt, kFast>
       <<<dim3((unsigned)(tiles * p.spans)), kThreads, 0, st>>>(p);
   return hipGetLastError();
 }
