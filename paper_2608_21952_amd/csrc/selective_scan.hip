@@ -39,83 +39,114 @@ int lanes_of(int64_t N) { return N <= 32 ? 8 : N <= 128 ? 16 : 32; }
 
 // ---------------------------------------------------------------------------- one token
 // kLanes lanes hold a channel, four states each: neighbouring ones (kWide: one 16-byte access, N a
-// multiple of 4) or every kLanes-th.  A lane takes kRun channels, whose states are all requested
-// before the first is used.
+// multiple of 4) or every kLanes-th.  A lane takes kRun channels, whose states are all requested first;
+// meanwhile a thread per channel forms what all its lanes need (delta or the tied decay, delta u), and
+// later its y.  What bounds it: the states' bytes, read and written once.
 template <int kLanes, int kRun, bool kWide>
 __global__ __launch_bounds__(kThreads) void scan_step_kernel(Args p, float* state) {
-  constexpr int kCh = kThreads / kLanes;
+  constexpr int kCh = kThreads / kLanes, kAll = kCh * kRun;
+  static_assert(kAll <= kThreads, "a thread per channel");
+  __shared__ float2 s_du[kAll];
+  __shared__ float s_y[kAll];
   const SelScan& a = p.s;
   const int nctile = p.group_tiles * (int)a.ngroups;
-  const Tile tile = tile_of(p, (int)(blockIdx.x % nctile), kCh * kRun);
+  const Tile tile = tile_of(p, (int)(blockIdx.x % nctile), kAll);
   const int64_t b = blockIdx.x / nctile;
   const int sub = threadIdx.x % kLanes, ch = threadIdx.x / kLanes;
   const int D = p.D, N = (int)a.dstate, P = (int)a.headdim;
   auto at = [&](int i) { return kWide ? sub * 4 + i : sub + kLanes * i; };
   auto value = [&](const void* t, int64_t off, int dtype) { return as_float(load_raw1(t, off, dtype), dtype); };
-
-  float h[kRun][4], u[kRun], dt[kRun], z[kRun];
-#pragma unroll
-  for (int r = 0; r < kRun; ++r) {
-    const int d = tile.first + r * kCh + ch;
-    const bool live = d < tile.end;
-    const float* sd = state + (b * D + d) * (int64_t)N;
+  // four values of a row of N, 0 behind its end
+  auto four = [&](const float* row, bool live, float (&v)[4]) {
     if (kWide) {
       float4 q = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-      if (live && at(0) < N) q = *reinterpret_cast<const float4*>(sd + at(0));
-      h[r][0] = q.x, h[r][1] = q.y, h[r][2] = q.z, h[r][3] = q.w;
+      if (live && at(0) < N) __builtin_memcpy(&q, row + at(0), 16);
+      v[0] = q.x, v[1] = q.y, v[2] = q.z, v[3] = q.w;
     } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) h[r][i] = live && at(i) < N ? sd[at(i)] : 0.0f;
+      for (int i = 0; i < 4; ++i) v[i] = live && at(i) < N ? row[at(i)] : 0.0f;
     }
-    u[r] = live ? value(a.u, b * a.ur.batch + d, a.dtype) : 0.0f;
-    dt[r] = live ? value(a.dt, b * a.dtr.batch + d / P, a.dt_dtype) : 0.0f;
-    z[r] = live && a.z ? value(a.z, b * a.zr.batch + d, a.dtype) : 0.0f;
-  }
-  float Bv[4], Cv[4];
+  };
+
+  float h[kRun][4], Bv[4], Cv[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int n = at(i);
-    Bv[i] = n < N ? value(a.B, b * a.Br.batch + (int64_t)tile.group * N + n, a.dtype) : 0.0f;
-    Cv[i] = n < N ? value(a.C, b * a.Cr.batch + (int64_t)tile.group * N + n, a.dtype) : 0.0f;
+  for (int r = 0; r < kRun; ++r) {
+    const int d = tile.first + r * kCh + ch;
+    four(state + (b * D + d) * (int64_t)N, d < tile.end, h[r]);
   }
+  auto column = [&](const void* t, int64_t row, float (&v)[4]) {
+    const char* q = static_cast<const char*>(t) + (row + (int64_t)tile.group * N) * (a.dtype == 0 ? 4 : 2);
+    if (kWide && a.dtype != 0) {
+      Raw<4> raw = {};
+      if (at(0) < N) __builtin_memcpy(raw.w, q + 2 * at(0), 8);
+      as_floats(raw, a.dtype, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = at(i) < N ? value(q, at(i), a.dtype) : 0.0f;
+    }
+  };
+  column(a.B, b * a.Br.batch, Bv);
+  column(a.C, b * a.Cr.batch, Cv);
+  // the channel of this thread
+  const int own = tile.first + (int)threadIdx.x;
+  const bool has = (int)threadIdx.x < kAll && own < tile.end;
+  float skip = 0.0f, gate = 1.0f;
+  if (has) {
+    const int hd = own / P;
+    const float u = value(a.u, b * a.ur.batch + own, a.dtype);
+    float delta = value(a.dt, b * a.dtr.batch + hd, a.dt_dtype);
+    if (a.z) gate = silu(value(a.z, b * a.zr.batch + own, a.dtype));
+    if (a.D) skip = a.D[hd] * u;
+    if (a.dt_bias) delta += a.dt_bias[hd];
+    if (a.dt_softplus) delta = softplus_fast(delta);
+    s_du[threadIdx.x] =
+        make_float2(a.tied ? __builtin_amdgcn_exp2f(delta * decay_rate(a.A[hd])) : delta, delta * u);
+  }
+  __syncthreads();
+  float y[kRun];
 #pragma unroll
   for (int r = 0; r < kRun; ++r) {
     const int d = tile.first + r * kCh + ch;
     const bool live = d < tile.end;
-    const int hd = live ? d / P : 0;
-    float delta = dt[r] + (a.dt_bias ? a.dt_bias[hd] : 0.0f);
-    if (a.dt_softplus) delta = softplus_fast(delta);
-    const float du = delta * u[r];
-    float tied = 0.0f, y = 0.0f;
-    if (a.tied) tied = __builtin_amdgcn_exp2f(delta * decay_rate(a.A[hd]));
+    const float2 du = s_du[r * kCh + ch];   // of a channel behind the group's end: not used
+    float m[4];
+    if (a.tied) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = du.x;
+    } else {
+      four(a.A + (int64_t)d * N, live, m);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m[i] = __builtin_amdgcn_exp2f(du.x * decay_rate(m[i]));
+    }
+    y[r] = 0.0f;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int n = at(i);
-      float m = tied;
-      if (!a.tied)
-        m = live && n < N ? __builtin_amdgcn_exp2f(delta * decay_rate(a.A[(int64_t)d * N + n])) : 0.0f;
-      h[r][i] = n < N ? __builtin_fmaf(m, h[r][i], du * Bv[i]) : 0.0f;
-      y = __builtin_fmaf(h[r][i], Cv[i], y);
+      h[r][i] = live && at(i) < N ? __builtin_fmaf(m[i], h[r][i], du.y * Bv[i]) : 0.0f;
+      y[r] = __builtin_fmaf(h[r][i], Cv[i], y[r]);
     }
-    y = lane_sum<kLanes>(y);
-    if (!live) continue;
-    float* sd = state + (b * D + d) * (int64_t)N;
-    if (kWide) {
-      if (at(0) < N)
-        *reinterpret_cast<float4*>(sd + at(0)) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
-    } else {
+    if (live) {
+      float* sd = state + (b * D + d) * (int64_t)N;
+      if (kWide) {
+        if (at(0) < N)
+          *reinterpret_cast<float4*>(sd + at(0)) = make_float4(h[r][0], h[r][1], h[r][2], h[r][3]);
+      } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (at(i) < N) sd[at(i)] = h[r][i];
+        for (int i = 0; i < 4; ++i)
+          if (at(i) < N) sd[at(i)] = h[r][i];
+      }
     }
-    if (sub == 0) {
-      y = __builtin_fmaf(a.D ? a.D[hd] : 0.0f, u[r], y);
-      if (a.z) y *= silu(z[r]);
-      const int64_t o = b * D + d;
-      if (a.dtype == 0) static_cast<float*>(a.y)[o] = y;
-      else if (a.dtype == 1) static_cast<_Float16*>(a.y)[o] = (_Float16)y;
-      else static_cast<bf16*>(a.y)[o] = (bf16)y;
-    }
+  }
+  lane_sums<kLanes, kRun>(y);
+  if (sub == 0)
+#pragma unroll
+    for (int r = 0; r < kRun; ++r) s_y[r * kCh + ch] = y[r];
+  __syncthreads();
+  if (has) {
+    const float v = (s_y[threadIdx.x] + skip) * gate;
+    const int64_t o = b * D + own;
+    if (a.dtype == 0) static_cast<float*>(a.y)[o] = v;
+    else if (a.dtype == 1) static_cast<_Float16*>(a.y)[o] = (_Float16)v;
+    else static_cast<bf16*>(a.y)[o] = (bf16)v;
   }
 }
 
