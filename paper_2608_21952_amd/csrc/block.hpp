@@ -100,6 +100,7 @@ struct Rows {
 struct ConvOut {
   void* y[3];
   int end[3];
+  int vec_end[3];   // the same in vectors of kVec columns, each output's last one begun anew (set by launch)
 };
 hipError_t launch_conv(int dtype, int width, int64_t batch, int64_t seqlen, int64_t channels,
                        const void* x, Rows xr, const float* weight, const float* bias, int silu,

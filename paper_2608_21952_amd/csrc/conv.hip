@@ -15,35 +15,51 @@ namespace ssdi8 {
 
 namespace {
 
-constexpr int kTokens = 16;   // of one thread's walk
+constexpr int kTokens = 32;   // of one thread's walk
 constexpr int kWaves = 4;     // walks of a workgroup, one behind the other
 
-// One vector of columns [c, c + kVec) of row `row` into the outputs that hold them.
-template <typename T>
-__device__ __forceinline__ void store_split(const ConvOut& o, int64_t row, int c, int D,
-                                            const float (&v)[kVec]) {
-  int begin = 0;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    const int end = o.end[i];
-    if (c >= begin && c < end) {
-      const int n = end - c < kVec ? end - c : kVec;
-      T* dst = static_cast<T*>(o.y[i]) + row * (end - begin) + (c - begin);
-      if (n == kVec) {
-        store_vec<T>(dst, kVec, v);
+// A thread's channels: vector `vec` of the columns, which never lies in two outputs.  The last vector of an
+// output is moved back to end with it, so that it is whole: the first `shift` of its channels are computed
+// twice, to the same values.  An output of fewer than kVec columns has one vector of n.
+template <typename T> struct Columns {
+  int c, n, shift;
+  T* y;           // its first column in the output
+  int64_t cols;   // of the output
+  __device__ __forceinline__ bool init(const ConvOut& o, int vec) {
+    if (vec >= o.vec_end[2]) return false;
+    // selects of values: of the arguments' addresses they would put the arguments into scratch memory
+    void *y0 = o.y[0], *y1 = o.y[1], *y2 = o.y[2];
+    asm("" : "+s"(y0), "+s"(y1), "+s"(y2));
+    int begin = 0, end = o.end[0], first = 0;
+    void* p = y0;
+    if (vec >= o.vec_end[0]) begin = o.end[0], end = o.end[1], first = o.vec_end[0], p = y1;
+    if (vec >= o.vec_end[1]) begin = o.end[1], end = o.end[2], first = o.vec_end[1], p = y2;
+    c = begin + (vec - first) * kVec;
+    n = kVec;
+    shift = 0;
+    if (c + kVec > end) {
+      if (end - begin >= kVec) {
+        shift = c + kVec - end;
+        c = end - kVec;
       } else {
-        for (int e = 0; e < kVec; ++e) {   // the columns that run past this output
-          const int col = c + e;
-          if (col >= D) break;
-          const int k = col < o.end[0] ? 0 : (col < o.end[1] ? 1 : 2);
-          const int lo = k == 0 ? 0 : o.end[k - 1];
-          static_cast<T*>(o.y[k])[row * (o.end[k] - lo) + (col - lo)] = (T)v[e];
-        }
+        n = end - c;
       }
     }
-    begin = end;
+    cols = end - begin;
+    y = static_cast<T*>(p) + (c - begin);
+    return true;
   }
-}
+  // to a state that is read too: its own channels alone
+  __device__ __forceinline__ void store_own(T* p, const float (&v)[kVec]) const {
+    if (n == kVec && shift == 0) {
+      store_vec<T>(p, kVec, v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (e >= shift && e < n) p[e] = (T)v[e];
+    }
+  }
+};
 
 template <int W>
 __device__ __forceinline__ void load_weights(const float* w, const float* bias, int c, int n,
@@ -56,91 +72,130 @@ __device__ __forceinline__ void load_weights(const float* w, const float* bias, 
   }
 }
 
+// The last W-1 rows before `len`, those before the sequence from the initial state (which may be the same
+// memory: all are read before the first is written, by the channels' one owner).
+template <typename T, int W>
+__device__ __forceinline__ void write_final(const Columns<T>& col, const T* xb, int64_t token, const T* init,
+                                            T* final_state, int64_t len, int64_t D) {
+  float last[W - 1][kVec];
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) {
+    const int64_t t = len - (W - 1) + j;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) last[j][e] = 0.0f;
+    if (t >= 0) load_vec<T>(xb + t * token, col.n, last[j]);
+    else if (init) load_vec<T>(init + (W - 1 + t) * D, col.n, last[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < W - 1; ++j) col.store_own(final_state + j * D, last[j]);
+}
+
+__device__ __forceinline__ int64_t length_of(const int* lengths, int64_t b, int64_t L) {
+  if (!lengths) return L;
+  return lengths[b] < 0 ? 0 : (lengths[b] < L ? lengths[b] : L);
+}
+
 template <typename T, int W, bool kSilu>
 __global__ __launch_bounds__(64 * kWaves) void conv_kernel(
     const T* __restrict__ x, Rows xr, const float* __restrict__ w, const float* __restrict__ bias,
-    const T* init, const int* __restrict__ lengths, ConvOut out, T* final_state, int64_t L, int D,
-    int nctile, int64_t nttile) {
+    const T* __restrict__ init, const int* __restrict__ lengths, ConvOut out, T* __restrict__ final_state,
+    int64_t L, int D, int nctile, int64_t nttile) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t bid = blockIdx.x;
   const int ct = (int)(bid % nctile);
   const int64_t tt = (bid / nctile) % nttile;
   const int64_t b = bid / nctile / nttile;
-  const int c = (ct * 64 + lane) * kVec;
-  if (c >= D) return;
-  const int n = D - c < kVec ? D - c : kVec;
+  Columns<T> col;
+  if (!col.init(out, ct * 64 + lane)) return;
+  const int c = col.c, n = col.n;
   const int64_t t0 = (tt * kWaves + wave) * kTokens;
-  int64_t len = L;
-  if (lengths) len = lengths[b] < 0 ? 0 : (lengths[b] < L ? lengths[b] : L);
+  if (t0 >= L && t0 > 0) return;
+  const int64_t len = length_of(lengths, b, L);
   const T* xb = x + b * xr.batch + c;
-  const bool first = t0 == 0;
-  if (t0 >= L && !first) return;
+  const T* ib = init ? init + b * (W - 1) * D + c : nullptr;
+  if (t0 == 0 && final_state)
+    write_final<T, W>(col, xb, xr.token, ib, final_state + b * (W - 1) * D + c, len, D);
+  if (L == 0) return;
 
   float wv[W][kVec], bv[kVec], win[W][kVec];
   load_weights<W>(w, bias, c, n, wv, bv);
+#pragma unroll
+  for (int e = 0; e < kVec; ++e) win[W - 1][e] = 0.0f;
   // rows t0 - (W-1) .. t0 - 1; those before the sequence from the initial state
 #pragma unroll
   for (int j = 0; j < W - 1; ++j) {
     const int64_t t = t0 - (W - 1) + j;
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) win[j][e] = 0.0f;
     if (t >= 0) {
-      if (t < len) {
-        load_vec<T>(xb + t * xr.token, n, win[j]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) win[j][e] = 0.0f;
-      }
-    } else if (init) {
-      load_vec<T>(init + (b * (W - 1) + (W - 1 + t)) * D + c, n, win[j]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) win[j][e] = 0.0f;
+      if (t < len) load_vec<T>(xb + t * xr.token, n, win[j]);
+    } else if (ib) {
+      load_vec<T>(ib + (W - 1 + t) * D, n, win[j]);
     }
   }
-  // the walk at token 0 also writes the final state: the only reader of the initial state, so that
-  // both may be the same memory
-  if (first && final_state) {
-    float last[W - 1][kVec];
+  T* dst = col.y + (b * L + t0) * col.cols;
+  auto token = [&](float (&y)[kVec]) {   // of the row in win[W - 1]
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j) {
-      const int64_t t = len - (W - 1) + j;
-      if (t >= 0) {
-        load_vec<T>(xb + t * xr.token, n, last[j]);
-      } else {
+    for (int e = 0; e < kVec; ++e) {
+      float v = bv[e];
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) last[j][e] = 0.0f;
+      for (int j = 0; j < W; ++j) v = __builtin_fmaf(wv[j][e], win[j][e], v);
+      y[e] = kSilu ? silu(v) : v;
 #pragma unroll
-        for (int i = 0; i < W - 1; ++i)   // t = i - (W - 1): row i of the window
-          if (t == i - (W - 1))
-#pragma unroll
-            for (int e = 0; e < kVec; ++e) last[j][e] = win[i][e];
-      }
+      for (int j = 0; j + 1 < W; ++j) win[j][e] = win[j + 1][e];
     }
+  };
+  if (n == kVec && t0 + kTokens <= len) {
+    // kAhead tokens' rows on their way during the arithmetic of those before them
+    constexpr int kAhead = 4;
+    RawVec<T> raw[2][kAhead];
+    const T* row = xb + t0 * xr.token;
+    auto request = [&](RawVec<T> (&r)[kAhead]) {
 #pragma unroll
-    for (int j = 0; j < W - 1; ++j)
-      store_vec<T>(final_state + (b * (W - 1) + j) * D + c, n, last[j]);
-  }
-#pragma unroll 4
-  for (int i = 0; i < kTokens; ++i) {
-    const int64_t t = t0 + i;
-    if (t >= L) break;
-    float y[kVec];
-    if (t < len) {
-      load_vec<T>(xb + t * xr.token, n, win[W - 1]);
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) {
-        float v = bv[e];
-#pragma unroll
-        for (int j = 0; j < W; ++j) v = __builtin_fmaf(wv[j][e], win[j][e], v);
-        y[e] = kSilu ? silu(v) : v;
-#pragma unroll
-        for (int j = 0; j + 1 < W; ++j) win[j][e] = win[j + 1][e];
+      for (int i = 0; i < kAhead; ++i) {
+        __builtin_memcpy(&r[i], row, sizeof(r[i]));
+        row += xr.token;
       }
-    } else {
+    };
+    request(raw[0]);
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) y[e] = 0.0f;
+    for (int i0 = 0; i0 < kTokens / kAhead; ++i0) {
+      if (i0 + 1 < kTokens / kAhead) request(raw[(i0 + 1) & 1]);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) win[W - 1][e] = (float)raw[i0 & 1][i].v[e];
+        float y[kVec];
+        token(y);
+        store_vec<T>(dst, kVec, y);
+        dst += col.cols;
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    store_split<T>(out, b * L + t, c, D, y);
+  } else {
+    for (int i = 0; i < kTokens && t0 + i < L; ++i) {
+      const bool in = t0 + i < len;
+      if (in) load_vec<T>(xb + (t0 + i) * xr.token, n, win[W - 1]);
+      float y[kVec];
+      token(y);
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) y[e] = in ? y[e] : 0.0f;
+      store_vec<T>(dst + i * col.cols, n, y);
+    }
   }
+}
+
+// The final states alone, where they are written over the initial ones that the kernel above reads.
+template <typename T, int W>
+__global__ __launch_bounds__(64) void conv_final_kernel(const T* __restrict__ x, Rows xr,
+                                                        const int* __restrict__ lengths, ConvOut out,
+                                                        T* state, int64_t L, int D, int nctile) {
+  const int64_t b = blockIdx.x / nctile;
+  Columns<T> col;
+  if (!col.init(out, (int)(blockIdx.x % nctile) * 64 + (int)threadIdx.x)) return;
+  T* sb = state + b * (W - 1) * D + col.c;
+  write_final<T, W>(col, x + b * xr.batch + col.c, xr.token, sb, sb, length_of(lengths, b, L), D);
 }
 
 template <typename T, int W, bool kSilu>
@@ -149,9 +204,9 @@ __global__ __launch_bounds__(64) void conv_step_kernel(const T* __restrict__ x, 
                                                        const float* __restrict__ bias, T* state,
                                                        ConvOut out, int D, int nctile) {
   const int64_t b = blockIdx.x / nctile;
-  const int c = ((int)(blockIdx.x % nctile) * 64 + (int)threadIdx.x) * kVec;
-  if (c >= D) return;
-  const int n = D - c < kVec ? D - c : kVec;
+  Columns<T> col;
+  if (!col.init(out, (int)(blockIdx.x % nctile) * 64 + (int)threadIdx.x)) return;
+  const int c = col.c, n = col.n;
   float wv[W][kVec], bv[kVec], win[W][kVec], y[kVec];
   T* sb = state + b * (W - 1) * D + c;
   load_vec<T>(x + b * x_row + c, n, win[W - 1]);
@@ -166,8 +221,19 @@ __global__ __launch_bounds__(64) void conv_step_kernel(const T* __restrict__ x, 
     y[e] = kSilu ? silu(v) : v;
   }
 #pragma unroll
-  for (int j = 0; j < W - 1; ++j) store_vec<T>(sb + (int64_t)j * D, n, win[j + 1]);
-  store_split<T>(out, b, c, D, y);
+  for (int j = 0; j < W - 1; ++j) col.store_own(sb + (int64_t)j * D, win[j + 1]);
+  col.store_own(col.y + b * col.cols, y);
+}
+
+// Sets the outputs' vectors; the waves that hold them all.
+int count_vectors(ConvOut& o) {
+  int vecs = 0, begin = 0;
+  for (int i = 0; i < 3; ++i) {
+    vecs += (o.end[i] - begin + kVec - 1) / kVec;
+    o.vec_end[i] = vecs;
+    begin = o.end[i];
+  }
+  return (vecs + 63) / 64;
 }
 
 template <typename F> hipError_t for_type(int dtype, int width, int silu, F&& f) {
@@ -192,26 +258,34 @@ template <typename F> hipError_t for_type(int dtype, int width, int silu, F&& f)
 
 hipError_t launch_conv(int dtype, int width, int64_t batch, int64_t seqlen, int64_t channels,
                        const void* x, Rows xr, const float* weight, const float* bias, int silu,
-                       const void* init, const int* lengths, const ConvOut& out, void* final_state,
+                       const void* init, const int* lengths, const ConvOut& outputs, void* final_state,
                        hipStream_t st) {
-  const int nctile = (int)((channels + 64 * kVec - 1) / (64 * kVec));
+  ConvOut out = outputs;
+  const int nctile = count_vectors(out);
   int64_t nttile = (seqlen + kTokens * kWaves - 1) / (kTokens * kWaves);
   if (nttile == 0) nttile = 1;   // no tokens: the states alone
   const int64_t grid = nctile * nttile * batch;
   return for_type(dtype, width, silu, [&](auto t, auto w, auto s) {
     using T = decltype(t);
-    conv_kernel<T, decltype(w)::value, decltype(s)::value>
-        <<<dim3((unsigned)grid), 64 * kWaves, 0, st>>>(
-            static_cast<const T*>(x), xr, weight, bias, static_cast<const T*>(init), lengths, out,
-            static_cast<T*>(final_state), seqlen, (int)channels, nctile, nttile);
+    constexpr int W = decltype(w)::value;
+    const bool over = final_state && final_state == init;
+    conv_kernel<T, W, decltype(s)::value><<<dim3((unsigned)grid), 64 * kWaves, 0, st>>>(
+        static_cast<const T*>(x), xr, weight, bias, static_cast<const T*>(init), lengths, out,
+        over ? nullptr : static_cast<T*>(final_state), seqlen, (int)channels, nctile, nttile);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !over) return e;
+    conv_final_kernel<T, W><<<dim3((unsigned)(nctile * batch)), 64, 0, st>>>(
+        static_cast<const T*>(x), xr, lengths, out, static_cast<T*>(final_state), seqlen, (int)channels,
+        nctile);
     return hipGetLastError();
   });
 }
 
 hipError_t launch_conv_step(int dtype, int width, int64_t batch, int64_t channels, const void* x,
                             int64_t x_row, const float* weight, const float* bias, int silu,
-                            void* state, const ConvOut& out, hipStream_t st) {
-  const int nctile = (int)((channels + 64 * kVec - 1) / (64 * kVec));
+                            void* state, const ConvOut& outputs, hipStream_t st) {
+  ConvOut out = outputs;
+  const int nctile = count_vectors(out);
   return for_type(dtype, width, silu, [&](auto t, auto w, auto s) {
     using T = decltype(t);
     conv_step_kernel<T, decltype(w)::value, decltype(s)::value>
