@@ -198,6 +198,10 @@ def lib() -> ctypes.CDLL:
     from . import _binding
     _binding.bind(addr(L.ssdi8_quantize_act), addr(L.ssdi8_ssd_workspace_size),
                   addr(L.ssdi8_ssd_chunk_scan), addr(L.ssdi8_decode_step), "cuda")
+    _binding.bind_block(addr(L.ssdi8_causal_conv), addr(L.ssdi8_causal_conv_step),
+                        addr(L.ssdi8_selective_scan_workspace_size), addr(L.ssdi8_selective_scan),
+                        addr(L.ssdi8_selective_scan_step), addr(L.ssdi8_gated_norm),
+                        addr(L.ssdi8_linear))
     _native = _binding
     _lib = L
     return L
@@ -683,6 +687,7 @@ def decode_step(x: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, Bq: torch.Te
 
 # ------------------------------------------------------------------- around the layer in a block
 _DTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.int8: I8}
+_CONV_ACT = (None, "none", "silu")
 _ACTIVATIONS = (torch.float32, torch.float16, torch.bfloat16)
 
 
@@ -776,6 +781,13 @@ def causal_conv(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torch.T
     init_state (B,W-1,D) the inputs before the first token, lengths (B) int32.
     split: up to three column counts; y is then a tuple of dense tensors, e.g. x, B, C of the layer.
     Returns y and, with final_state, the last W-1 inputs (B,W-1,D)."""
+    if y is None and stream is None and activation in _CONV_ACT and _plain(x):
+        r = _native.conv(x, weight, bias, ACT[activation], split, init_state, lengths,
+                         int(final_state), _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_causal_conv")
+            return {"y": r[1], "final_state": r[2]} if final_state else {"y": r[1]}
     _activation_type(x, "x", 3)
     B, L, D = x.shape
     _rows(x, "x", x.dtype, (B, L, D))
@@ -800,6 +812,12 @@ def causal_conv_step(x: torch.Tensor, weight: torch.Tensor, state: torch.Tensor,
                      split=None, y=None, stream=None):
     """One token of causal_conv (ssdi8_causal_conv_step): x (B,D); state (B,W-1,D), the inputs before the
     token, is updated in place.  Returns y (B,D), or the tuple of its columns with split."""
+    if y is None and stream is None and activation in _CONV_ACT and _plain(x):
+        r = _native.conv_step(x, weight, state, bias, ACT[activation], split, _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_causal_conv_step")
+            return r[1]
     _activation_type(x, "x", 2)
     B, D = x.shape
     _rows(x, "x", x.dtype, (B, D))
@@ -857,6 +875,13 @@ def selective_scan(u: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: torch.
     u's type or fp32 with ch a multiple of H, A (ch,N) or, one decay per head, (H); B, C (b,L,G,N),
     D, dt_bias (H), init_state (b,ch,N) fp32, lengths (b) int32.  Rows are dense, their strides any.
     Returns y (b,L,ch) and, with final_state, the state after the last token (b,ch,N) fp32."""
+    if y is None and workspace is None and stream is None and _plain(u):
+        r = _native.sel_scan(u, dt, A, None, B, C, D, z, dt_bias, int(dt_softplus), init_state,
+                             lengths, int(final_state), _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_selective_scan")
+            return {"y": r[1], "final_state": r[2]} if final_state else {"y": r[1]}
     _activation_type(u, "u", 3)
     d, a, y = _sel_scan(u, dt, A, B, C, D, z, dt_bias, dt_softplus, y, stream)
     state = (d.batch, u.shape[2], d.dstate)
@@ -891,6 +916,13 @@ def selective_scan_step(u: torch.Tensor, dt: torch.Tensor, A: torch.Tensor, B: t
                         stream=None) -> torch.Tensor:
     """One token of selective_scan (ssdi8_selective_scan_step): u, z (b,ch), dt (b,H), B, C (b,G,N); state
     (b,ch,N) fp32 is updated in place.  Returns y (b,ch)."""
+    if y is None and stream is None and _plain(u):
+        r = _native.sel_scan_step(u, dt, A, state, B, C, D, z, dt_bias, int(dt_softplus),
+                                  _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_selective_scan_step")
+            return r[1]
     _activation_type(u, "u", 2)
     d, a, y = _sel_scan(u, dt, A, B, C, D, z, dt_bias, dt_softplus, y, stream)
     a.final_state = _param(state, "state", (d.batch, u.shape[1], d.dstate))
@@ -918,6 +950,16 @@ def gated_norm(x: torch.Tensor, weight: torch.Tensor, *, z: Optional[torch.Tenso
     """RMS norm with an optional gate and residual (ssdi8_gated_norm): x, z, residual (..., D), weight
     (D); x and z may be columns of wider rows.  Returns y and, with a residual, the sum x + residual
     (in residual_out, which may be the residual itself, or a new tensor)."""
+    if stream is None and _plain(x):
+        r = _native.norm(x, weight, z, residual, eps, groups, int(norm_before_gate), y, residual_out,
+                         _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_gated_norm")
+            out = {"y": r[1] if y is None else y}
+            if residual is not None:
+                out["residual"] = r[2] if residual_out is None else residual_out
+            return out
     lead = tuple(x.shape[:-1])
     xr = _flat(x, "x")
     _activation_type(xr, "x", 2)
@@ -956,6 +998,14 @@ def linear(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torch.Tensor
     weight (O,K) fp16 or bf16, or int8 codes with x_scale (one step per row of x) and w_scale (O);
     bias (O) fp32, activation None, "silu", "gelu" or "softplus", residual (..., O) of y's type.
     y (..., O) has x's type (int8: fp16) or is fp32 (y_dtype)."""
+    if y is None and stream is None and activation in ACT and (y_dtype is None or y_dtype in _DTYPES) \
+            and _plain(x):
+        r = _native.linear(x, weight, bias, ACT[activation], residual, x_scale, w_scale,
+                           -1 if y_dtype is None else _DTYPES[y_dtype], _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_linear")
+            return r[1]
     lead = tuple(x.shape[:-1])
     xr = _flat(x, "x")
     if x.dtype not in (torch.float16, torch.bfloat16, torch.int8):
