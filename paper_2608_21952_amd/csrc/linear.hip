@@ -254,14 +254,17 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
   // columns, the same ones of every row
   float* out = reinterpret_cast<float*>(lds) + wave * 32 * kOutRow;
   const int64_t wm0 = m0 + wm * kTM * 32, wn0 = n0 + wn * kTN * 32;
-  constexpr int kPer = kTN * 32 / kVec;    // lanes of a row on the way out
-  constexpr int kRows = 64 / kPer;
-  const int oc = (lane % kPer) * kVec;
-  const int64_t cc = wn0 + oc;
-  const int cn = cc >= a.n ? 0 : (a.n - cc < kVec ? (int)(a.n - cc) : kVec);
+  constexpr int kPer = kTN * 32 / kVec;    // vectors of a row on the way out
+  constexpr bool kSame = 64 % kPer == 0;   // a lane has the same columns in every row
+  static_assert(32 * kPer % 64 == 0, "whole waves on the way out");
   float bias[kVec] = {}, ws[kVec] = {};
-  if (a.bias) load_vec<float>(a.bias + cc, cn, bias);
-  if constexpr (std::is_same_v<K, I8>) load_vec<float>(a.w_scale + cc, cn, ws);
+  auto columns = [&](int64_t c, int n) {
+    if (n <= 0) return;
+    if (a.bias) load_vec<float>(a.bias + c, n, bias);
+    if constexpr (std::is_same_v<K, I8>) load_vec<float>(a.w_scale + c, n, ws);
+  };
+  if (kSame) columns(wn0 + lane % kPer * kVec, (int)(a.n - wn0 - lane % kPer * kVec < kVec
+                                                        ? a.n - wn0 - lane % kPer * kVec : kVec));
 #pragma unroll
   for (int i = 0; i < kTM; ++i) {
 #pragma unroll
@@ -274,9 +277,11 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
     // the wave's own rows: no other wave reads or writes them
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int r0 = 0; r0 < 32; r0 += kRows) {
-      const int r = r0 + lane / kPer;
-      const int64_t mm = wm0 + i * 32 + r;
+    for (int k = 0; k < 32 * kPer / 64; ++k) {
+      const int r = (k * 64 + lane) / kPer, oc = (k * 64 + lane) % kPer * kVec;
+      const int64_t mm = wm0 + i * 32 + r, cc = wn0 + oc;
+      const int cn = cc >= a.n ? 0 : (a.n - cc < kVec ? (int)(a.n - cc) : kVec);
+      if (!kSame) columns(cc, cn);
       float v[kVec];
       const float4 lo = *reinterpret_cast<const float4*>(out + r * kOutRow + oc);
       const float4 hi = *reinterpret_cast<const float4*>(out + r * kOutRow + oc + 4);

@@ -304,6 +304,21 @@ def test_linear(ssdi8, M, O, K, dtype, bias, act, res, y32, before):
     R.assert_within(got, y, R.rounded(yd, y, e), "y")
 
 
+@pytest.mark.parametrize("M,O", [(4090, 4090), (4090, 3060), (4090, 2040), (2040, 2040), (1000, 1000)])
+@pytest.mark.parametrize("K,dtype", [(80, F16), (321, "i8")])
+def test_linear_tiles(ssdi8, M, O, K, dtype):
+    """A size for each tile of the larger products (256 x 256, 192, 128, 128 x 128, 64 x 64), whole value
+    by whole value: small integers, whose products and sums every type holds exactly."""
+    r = Draw(M + O)
+    x, w = (r.uniform(-2.5, 2.5, *s).round() for s in ((M, K), (O, K)))
+    b, rr = r.uniform(-9, 9, O).round(), r.uniform(-9, 9, M, O).round()
+    kind = torch.int8 if dtype == "i8" else dtype
+    kw = dict(x_scale=torch.ones(M, device="cuda"), w_scale=torch.ones(O, device="cuda")) if dtype == "i8" else {}
+    got = ssdi8.linear(x.to(kind).cuda(), w.to(kind).cuda(), bias=dev(b), residual=dev(rr), y_dtype=F32, **kw)
+    want = x.cuda().double() @ w.cuda().double().t() + dev(b) + dev(rr)
+    assert torch.equal(got.double(), want)
+
+
 @pytest.mark.parametrize("M", [3, 80])
 def test_linear_writes_its_columns_only(ssdi8, M):
     """y and the residual as columns of wider rows, y over the residual; NaN in a row of x stays there."""
