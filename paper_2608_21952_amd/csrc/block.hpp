@@ -56,15 +56,14 @@ __device__ __forceinline__ float fast_exp(float v) {
 __device__ __forceinline__ float silu(float v) {
   return v * __builtin_amdgcn_rcpf(1.0f + fast_exp(-v));
 }
-// log(1 + exp(v)) in fp32, v itself above 20 (there the difference is below half an ulp).  With
-// z = exp(-|v|) and u = fl(1 + z), log(u) + (z - (u - 1)) takes back the rounding of u: the exact term is
+// log(1 + exp(v)) in fp32 (v itself above 17: what is added there is below half an ulp).  With z = exp(-|v|)
+// and u = fl(1 + z), log(u) + (z - (u - 1)) takes back the rounding of u: the exact term is
 // (z - (u - 1)) / u, and what the missing division leaves is z (z - (u - 1)), below an ulp of the result.
 __device__ __forceinline__ float softplus_fast(float v) {
   const float z = fast_exp(-__builtin_fabsf(v));
   const float u = 1.0f + z;
   const float l1p = __builtin_fmaf(0.693147180559945309f, __builtin_amdgcn_logf(u), z - (u - 1.0f));
-  const float s = __builtin_fmaxf(v, 0.0f) + l1p;
-  return v > 20.0f || v != v ? v : s;
+  return __builtin_fmaxf(v, 0.0f) + l1p;   // a NaN stays one through z
 }
 
 // Sums over kLanes neighbouring lanes (a power of two) of kCount values, in every one of the lanes.

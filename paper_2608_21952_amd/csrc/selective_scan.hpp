@@ -85,25 +85,45 @@ __device__ __forceinline__ float decay_rate(float A) {
   return a == -__builtin_inff() ? -__FLT_MAX__ : a;
 }
 
-// States [n0, n0 + kS) of a row of N, 0 behind its end.
-template <int kS> __device__ __forceinline__ void load_states(const float* row, int n0, int N, float (&h)[kS]) {
-  if (n0 + kS <= N) {
-    __builtin_memcpy(h, row + n0, sizeof(h));
-  } else {
+// A lane's kS states lie in pieces of up to four neighbouring ones, the pieces of a channel's kLanes lanes side
+// by side: 16 lanes then read 256 bytes of a row of B in a line, where eight states in a line per lane put
+// every second lane on the same banks.
+template <int kLanes, int kS> struct States {
+  static constexpr int kPiece = kS < 4 ? kS : 4, kPieces = kS / kPiece;
+  static __device__ __forceinline__ int at(int sub, int piece) { return (piece * kLanes + sub) * kPiece; }
+  // of a row of N, 0 behind its end
+  static __device__ __forceinline__ void load(const float* row, int sub, int N, float (&h)[kS]) {
 #pragma unroll
-    for (int i = 0; i < kS; ++i) h[i] = n0 + i < N ? row[n0 + i] : 0.0f;
-  }
-}
-template <int kS>
-__device__ __forceinline__ void store_states(float* row, int n0, int N, const float (&h)[kS]) {
-  if (n0 + kS <= N) {
-    __builtin_memcpy(row + n0, h, sizeof(h));
-  } else {
+    for (int k = 0; k < kPieces; ++k) {
+      const int n0 = at(sub, k);
+      if (n0 + kPiece <= N) {
+        __builtin_memcpy(&h[k * kPiece], row + n0, 4 * kPiece);
+      } else {
 #pragma unroll
-    for (int i = 0; i < kS; ++i)
-      if (n0 + i < N) row[n0 + i] = h[i];
+        for (int i = 0; i < kPiece; ++i) h[k * kPiece + i] = n0 + i < N ? row[n0 + i] : 0.0f;
+      }
+    }
   }
-}
+  static __device__ __forceinline__ void store(float* row, int sub, int N, const float (&h)[kS]) {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k) {
+      const int n0 = at(sub, k);
+      if (n0 + kPiece <= N) {
+        __builtin_memcpy(row + n0, &h[k * kPiece], 4 * kPiece);
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i)
+          if (n0 + i < N) row[n0 + i] = h[k * kPiece + i];
+      }
+    }
+  }
+  // of a row of B or C in LDS
+  static __device__ __forceinline__ void take(const float* row, int sub, float* v) {
+#pragma unroll
+    for (int k = 0; k < kPieces; ++k)
+      __builtin_memcpy(v + k * kPiece, __builtin_assume_aligned(row + at(sub, k), 4 * kPiece), 4 * kPiece);
+  }
+};
 
 // Where channel pair `pair` of a token's row of kCh channels lies.  With vectors of eight channels the low two
 // bits of its place are exchanged so that the 16 lanes of an access, neighbouring vectors and tokens, touch
@@ -228,7 +248,8 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   const int64_t t_end = t_begin + p.span < L ? t_begin + p.span : L;
 
   // the states of this lane
-  const int ch = tid / kLanes, sub = tid % kLanes, n0 = sub * kS;
+  const int ch = tid / kLanes, sub = tid % kLanes;
+  using St = States<kLanes, kS>;
   const int d = tile.first + ch;
   const bool live = d < tile.end;
   float rate[kS], h[kS] = {};
@@ -240,20 +261,20 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   for (int i = 0; i < kS; ++i) rate[i] = 0.0f;
   if (live) {
     if constexpr (!kTied) {
-      load_states<kS>(a.A + (int64_t)d * N, n0, N, rate);
+      St::load(a.A + (int64_t)d * N, sub, N, rate);
 #pragma unroll
       for (int i = 0; i < kS; ++i) rate[i] = decay_rate(rate[i]);
     }
     if constexpr (kStates) {
       if (span == 0) {   // the initial state into the workspace: the final one may overwrite it
         float init[kS] = {};
-        if (a.init) load_states<kS>(a.init + state_row, n0, N, init);
-        store_states<kS>(ws_state, n0, N, init);
+        if (a.init) St::load(a.init + state_row, sub, N, init);
+        St::store(ws_state, sub, N, init);
       }
     } else if (p.spans == 1) {
-      if (a.init) load_states<kS>(a.init + state_row, n0, N, h);
+      if (a.init) St::load(a.init + state_row, sub, N, h);
     } else {
-      load_states<kS>(ws_state, n0, N, h);
+      St::load(ws_state, sub, N, h);
       const float* decays = ws_decay + b * p.spans * D + d;
       constexpr int kAhead = 4;   // spans requested at a time
       for (int c = 0; c < span; c += kAhead) {
@@ -262,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
         for (int k = 0; k < kAhead; ++k) {
           const int at = c + k < span ? c + k : span - 1;
           dec[k] = decays[(int64_t)at * D];
-          load_states<kS>(ws_state + (at + 1) * ws_span, n0, N, end[k]);
+          St::load(ws_state + (at + 1) * ws_span, sub, N, end[k]);
         }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
@@ -403,11 +424,11 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
       if (a.dt_softplus)
 #pragma unroll
         for (int i = 0; i < kSV; ++i) dl[i] = softplus_fast(dl[i]);
+      if (!valid)
+#pragma unroll
+        for (int i = 0; i < kSV; ++i) dl[i] = 0.0f, u[i] = 0.0f;
 #pragma unroll
       for (int i = 0; i < kSV; ++i) {
-        const bool in = valid && (kFast || i < nc);
-        dl[i] = in ? dl[i] : 0.0f;
-        u[i] = in ? u[i] : 0.0f;
         const float m = kTied ? __builtin_amdgcn_exp2f(dl[i] * head_rate[i]) : dl[i];
         dl[i] *= u[i];
         ml[i] = m;
@@ -464,9 +485,9 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
       for (int j = 0; j < kGroup; ++j) {
         g[j].du = *reinterpret_cast<const float2*>(
             &s_du[s0 + j][4 * pair_slot<kCh, kSV>(s0 + j, ch / 2) + 2 * (ch & 1)]);
-        __builtin_memcpy(g[j].B, __builtin_assume_aligned(&s_B[s0 + j][n0], kS > 2 ? 16 : 8), sizeof(g[j].B));
+        St::take(s_B[s0 + j], sub, g[j].B);
         if constexpr (!kStates)
-          __builtin_memcpy(g[j].C, __builtin_assume_aligned(&s_C[s0 + j][n0], kS > 2 ? 16 : 8), sizeof(g[j].C));
+          St::take(s_C[s0 + j], sub, g[j].C);
       }
     };
     take(0, q[0]);
@@ -517,8 +538,9 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
         if (a.z)
 #pragma unroll
           for (int i = 0; i < kSV; ++i) done[i] *= silu(z[i]);
+        if (!valid)
 #pragma unroll
-        for (int i = 0; i < kSV; ++i) done[i] = valid ? done[i] : 0.0f;
+          for (int i = 0; i < kSV; ++i) done[i] = 0.0f;
       }
     }
   }
@@ -526,9 +548,9 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   if (!live) return;
   if constexpr (kStates) {
     if (sub == 0) ws_decay[(b * p.spans + span) * D + d] = decay;
-    store_states<kS>(ws_state + (span + 1) * ws_span, n0, N, h);
+    St::store(ws_state + (span + 1) * ws_span, sub, N, h);
   } else if (a.final_state && span == p.spans - 1) {
-    store_states<kS>(a.final_state + state_row, n0, N, h);
+    St::store(a.final_state + state_row, sub, N, h);
   }
 }
 
