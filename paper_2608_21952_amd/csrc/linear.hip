@@ -9,8 +9,8 @@
 // c ^ (r / 2 % 8), so that the 16 lanes that a fragment read serves at a time touch every bank once.  w is
 // the first operand: a lane then holds four consecutive columns of a row, and the tile leaves through LDS
 // in whole lines.
-// Few rows (linear_rows): bound by the bytes of w.  A workgroup takes 16 rows of w, its waves share k by
-// lines of 128 bytes, each straight from memory into the matrix instruction's registers, and their sums
+// Few rows (linear_rows): bound by the bytes of w.  A workgroup takes 16 or 32 rows of w, its waves share k
+// by lines of 128 bytes, each straight from memory into the matrix instruction's registers, and their sums
 // meet in LDS.
 // What lies behind a row's end in its last k-tile or line becomes 0 in both operands; rows may start at any
 // element.
@@ -308,49 +308,72 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
 
 constexpr int kRowLine = 128;
 
-// 16 rows of w by kMT x 16 rows of x per workgroup of kWaves waves.
-template <typename K, int kMT, int kWaves>
+// kNT x 16 rows of w by kMT x 16 rows of x per workgroup of kWaves waves.
+template <typename K, int kNT, int kMT, int kWaves>
 __global__ __launch_bounds__(64 * kWaves) void linear_rows(LinearArgs a) {
   typedef typename K::T T;
   typedef std::conditional_t<std::is_same_v<K, I8>, int, float> Sum;
-  __shared__ Sum part[kWaves][kMT][256];
+  __shared__ Sum part[kWaves][kNT * kMT][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * kMT);
+  const int64_t n0 = (int64_t)blockIdx.x * (16 * kNT);
   const int64_t kbytes = a.k * (int64_t)sizeof(T);
-  const int lines = (int)((kbytes + kRowLine - 1) / kRowLine);
+  const int whole = (int)(kbytes / kRowLine), lines = (int)((kbytes + kRowLine - 1) / kRowLine);
   const int fr = lane & 15, fk = lane >> 4;
-  const int64_t wr = n0 + fr < a.n ? n0 + fr : a.n - 1;
-  const char* wrow = static_cast<const char*>(a.w) + wr * a.w_row * (int64_t)sizeof(T);
-  const char* xrow[kMT];
+  const char *wrow[kNT], *xrow[kMT];
+#pragma unroll
+  for (int j = 0; j < kNT; ++j) {
+    const int64_t n = n0 + j * 16 + fr < a.n ? n0 + j * 16 + fr : a.n - 1;
+    wrow[j] = static_cast<const char*>(a.w) + n * a.w_row * (int64_t)sizeof(T) + fk * 16;
+  }
 #pragma unroll
   for (int i = 0; i < kMT; ++i) {
-    const int64_t m = m0 + i * 16 + fr < a.m ? m0 + i * 16 + fr : a.m - 1;
-    xrow[i] = static_cast<const char*>(a.x) + m * a.x_row * (int64_t)sizeof(T);
+    const int64_t m = i * 16 + fr < a.m ? i * 16 + fr : a.m - 1;
+    xrow[i] = static_cast<const char*>(a.x) + m * a.x_row * (int64_t)sizeof(T) + fk * 16;
   }
-  typename K::Acc16 acc[kMT] = {};
-#pragma unroll 4
-  for (int l = wave; l < lines; l += kWaves) {
+  typename K::Acc16 acc[kNT][kMT] = {};
+  auto line = [&](int l, auto inside) {
+    constexpr bool kInside = decltype(inside)::value;   // the line ends before the row does
+    uint4 wv[2][kNT], xv[2][kMT];
+    auto get = [&](const char* row, int s) {
+      const int64_t at = (int64_t)l * kRowLine + s * 64;
+      uint4 v;
+      if constexpr (kInside) __builtin_memcpy(&v, row + at, 16);
+      else v = load_chunk<T>(row + at, 0, kbytes - at - fk * 16);
+      return v;
+    };
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      const int64_t at = (int64_t)l * kRowLine + s * 64 + fk * 16;
-      const uint4 wv = load_chunk<T>(wrow, at, kbytes);
 #pragma unroll
-      for (int i = 0; i < kMT; ++i)
-        acc[i] = K::mma16(wv, load_chunk<T>(xrow[i], at, kbytes), acc[i]);
+      for (int j = 0; j < kNT; ++j) wv[s][j] = get(wrow[j], s);
+#pragma unroll
+      for (int i = 0; i < kMT; ++i) xv[s][i] = get(xrow[i], s);
     }
-  }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int j = 0; j < kNT; ++j)
+#pragma unroll
+        for (int i = 0; i < kMT; ++i) acc[j][i] = K::mma16(wv[s][j], xv[s][i], acc[j][i]);
+  };
+  int l = wave;
+  constexpr int kUnroll = 8 / (kNT + kMT) > 1 ? 8 / (kNT + kMT) : 1;
+#pragma unroll kUnroll
+  for (; l < whole; l += kWaves) line(l, std::true_type());
+  if (l < lines) line(l, std::false_type());
   // a lane holds row fr of x, columns 4 fk + (0..3)
 #pragma unroll
-  for (int i = 0; i < kMT; ++i)
+  for (int j = 0; j < kNT; ++j)
 #pragma unroll
-    for (int e = 0; e < 4; ++e) part[wave][i][fr * 16 + fk * 4 + e] = acc[i][e];
+    for (int i = 0; i < kMT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) part[wave][j * kMT + i][fr * 16 + fk * 4 + e] = acc[j][i][e];
   __syncthreads();
-  for (int o = tid; o < kMT * 256; o += 64 * kWaves) {
-    const int i = o >> 8, r = (o >> 4) & 15, c = o & 15;
-    const int64_t m = m0 + i * 16 + r, n = n0 + c;
+  for (int o = tid; o < kNT * kMT * 256; o += 64 * kWaves) {
+    const int tile = o >> 8, r = (o >> 4) & 15, c = o & 15;
+    const int64_t m = tile % kMT * 16 + r, n = n0 + tile / kMT * 16 + c;
     Sum sum = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) sum += part[w][i][o & 255];
+    for (int w = 0; w < kWaves; ++w) sum += part[w][tile][o & 255];
     if (m >= a.m || n >= a.n) continue;
     float v = (float)sum;
     if constexpr (std::is_same_v<K, I8>) v *= a.x_scale[m] * a.w_scale[n];
@@ -376,13 +399,20 @@ hipError_t run_tile(const LinearArgs& a, hipStream_t st) {
 }
 
 template <typename K> hipError_t run(const LinearArgs& a, hipStream_t st) {
-  if (a.m <= 64) {
-    const unsigned nt = (unsigned)((a.n + 15) / 16);
-    if (a.m <= 16) linear_rows<K, 1, 8><<<dim3(nt, 1), 512, 0, st>>>(a);
-    else if (a.m <= 32) linear_rows<K, 2, 8><<<dim3(nt, 1), 512, 0, st>>>(a);
-    else linear_rows<K, 4, 8><<<dim3(nt, 1), 512, 0, st>>>(a);
+  // Few rows.  Up to 16, one matrix tile of x: 8 x 10496 x 2560 bf16 13.1 us with 16 rows of w per workgroup,
+  // 15.2 with 32 (8 x 2560 x 5120 9.2 / 14.6).  Up to 32, twice the rows of w where they still fill the card:
+  // 24 x 5120 x 2560 int8 8.0 / 6.9.  Up to 64, until the tiles below do: 64 x 2560 x 5120 24.9 (tiles 29.2),
+  // 40 x 10496 x 2560 28.6 (tiles 16.9).
+  auto rows = [&](auto most, auto tiles) {
+    constexpr int kMT = decltype(most)::value, kNT = decltype(tiles)::value;
+    linear_rows<K, kNT, kMT, 8><<<dim3((unsigned)((a.n + 16 * kNT - 1) / (16 * kNT))), 512, 0, st>>>(a);
     return hipGetLastError();
-  }
+  };
+  using One = std::integral_constant<int, 1>;
+  using Two = std::integral_constant<int, 2>;
+  if (a.m <= 16) return rows(One(), One());
+  if (a.m <= 32) return a.n >= 4096 ? rows(Two(), Two()) : rows(Two(), One());
+  if (a.m <= 64 && a.n < 64 * 128) return rows(std::integral_constant<int, 4>(), One());
   // The tile whose rounds over the card's 256 CUs cost least: rounds * area / rate, the rates (of the
   // largest tile's) as 8192^3 in bf16 measured them: 898 us with 256 x 256, 986 with 256 x 192, 1030 with
   // 256 x 128, 1108 with 128 x 128, 1700 with 64 x 64.  Where another than the largest wins: 16384 x 768 x
