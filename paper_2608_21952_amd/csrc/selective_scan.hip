@@ -3,8 +3,7 @@
 //   s[t, n]  = exp(delta[t] A[d, n]) s[t-1, n] + delta[t] u[t, d] B[t, g, n]
 //   y[t, d]  = (sum_n C[t, g, n] s[t, n] + D[h] u[t, d]) silu(z[t, d])
 // with one decay per channel and state (A [d, n]) or per head (`tied`, A [h]), any length, from a
-// given state.  The steps of several orders of magnitude more tokens than lanes are serial per
-// (channel, state), so the work is laid over channels and states:
+// given state.  A (channel, state)'s tokens are serial, so the work is laid over channels and states:
 //   kLanes neighbouring lanes hold a channel, each kS of its states in registers; a workgroup of 256
 //   threads holds 256 / kLanes channels and walks tiles of kTile tokens.  A tile's inputs come in
 //   coalesced, are turned once into delta (or the tied decay) and delta u, and into fp32 B and C, in
@@ -14,8 +13,12 @@
 // reaches from zero and its decay (the sum of delta, or the tied decays' product); in the second the
 // workgroup of a span joins those of the spans before it and walks its own.
 //
-// What bounds it: the vector unit.  Per (token, channel, state) one exponential on the quarter-rate
-// unit and four full-rate operations, or three operations alone where the decay is tied.
+// What bounds it: the vector unit.  Per (token, channel, state) one exponential at half rate and four
+// full-rate operations (three alone where the decay is tied), 61 us over the card's 1024 SIMDs for 8 x 2048 x
+// 1536 x 16; softplus, gate and conversions of every element take about as long as half of that, the sums
+// over a channel's lanes a quarter.  Measured there 196 us (fp16 with gate; 1.5 workgroups per CU, so that the
+// fuller ones decide), 503 us for 4 x 4096 x 5120 x 16 in bf16, 220 us for one fp32 prompt of 16384 x 1536, 36 us
+// for three remainders of 201 tokens, 24 heads of 64 x 128.
 //
 // Everything is held in fp32; y is rounded once.  Tokens at or behind a sequence's length count as
 // delta = 0 and u = 0, which leave the state as it is, and are not read.
@@ -41,7 +44,8 @@ int lanes_of(int64_t N) { return N <= 32 ? 8 : N <= 128 ? 16 : 32; }
 // kLanes lanes hold a channel, four states each: neighbouring ones (kWide: one 16-byte access, N a
 // multiple of 4) or every kLanes-th.  A lane takes kRun channels, whose states are all requested first;
 // meanwhile a thread per channel forms what all its lanes need (delta or the tied decay, delta u), and
-// later its y.  What bounds it: the states' bytes, read and written once.
+// later its y.  What bounds it: the states' bytes, read and written once: 128 x 5120 channels x 128 states in
+// 127 us, 5.3 TB/s, the rate of a large copy.
 template <int kLanes, int kRun, bool kWide>
 __global__ __launch_bounds__(kThreads) void scan_step_kernel(Args p, float* state) {
   constexpr int kCh = kThreads / kLanes, kAll = kCh * kRun;
@@ -155,8 +159,9 @@ __global__ __launch_bounds__(kThreads) void scan_step_kernel(Args p, float* stat
 int sel_scan_spans(int64_t batch, int64_t seqlen, int64_t channels, int64_t groups, int64_t dstate) {
   const int64_t wgs = batch * tiles_of(channels, groups, kThreads / lanes_of(dstate));
   // Uncut from a workgroup per CU on: a cut costs the walk a second time, less what only y needs (8 x 2048 x
-  // 1536 x 16, 384 workgroups: 191 us uncut, 217 in 2 spans; 4 x 4096 x 5120, 640: 566 and 632).  Below, three
-  // workgroups per CU (1 x 16384 x 1536, 48: 905 us uncut, 232 in 16 spans, 230 in 32), of 128 tokens or more.
+  // 1536 x 16, 384 workgroups: 196 us uncut, 199 in 2 spans; 4 x 4096 x 5120, 640: 503 and 584; against it, a
+  // tied decay of 80 heads over 2000 tokens, 320: 307 and 268).  Below, three workgroups per CU (1 x 16384 x
+  // 1536 fp32, 48: 905 us uncut; 265, 220 and 240 in 10, 16 and 21 spans), of 128 tokens or more.
   if (wgs >= 256 || wgs == 0) return 1;
   const int64_t most = (seqlen + 127) / 128;
   int64_t spans = 768 / wgs;

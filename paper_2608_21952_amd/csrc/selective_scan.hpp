@@ -214,10 +214,12 @@ __device__ __forceinline__ Tile tile_of(const Args& p, int ct, int channels) {
 // then the spans' decays [b, spans, d].
 // kTile: tokens of a tile.  kSV: channels of a thread's part of a tile, so that all threads have one.
 template <int kLanes, int kS, int kTile, int kSV, bool kTied, bool kStates, int kType, int kDt, bool kFast>
-__global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
+__global__ __launch_bounds__(kThreads, kS == 2 && kFast ? 3 : 1) void scan_kernel(Args p) {
   constexpr int kCh = kThreads / kLanes;            // channels of a workgroup
   constexpr int kN = kLanes * kS;                   // states, padded
-  constexpr int kGroup = kS > 4 ? 2 : kS == 4 ? 4 : 8, kPair = 2 * kGroup;
+  // Tokens whose operands are read together; with two states per lane as many as leave three waves per SIMD
+  // (4 x 4096 x 5120 bf16: 565 us with eight and two waves, 503 with four and three; 8 x 2048 x 1536: 188, 196)
+  constexpr int kGroup = kS > 4 || (kType == 0 && kS == 2) ? 2 : 4, kPair = 2 * kGroup;
   constexpr int kVecs = kCh / kSV;                  // vectors of a token's channels
   constexpr int kBcVecs = kTile * (kN / kVec);      // vectors of a tile of B (or C)
   constexpr int kBc = (kBcVecs + kThreads - 1) / kThreads;
@@ -230,6 +232,7 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   __shared__ __attribute__((aligned(16))) float s_B[kTile][kN];
   __shared__ __attribute__((aligned(16))) float s_C[kStates ? 1 : kTile][kStates ? 4 : kN];
 
+  __shared__ __attribute__((aligned(16))) float s_head[3][kCh];
   const SelScan& a = p.s;
   const int dtype = kType >= 0 ? kType : a.dtype, dt_dtype = kDt >= 0 ? kDt : a.dt_dtype;
   const int tid = threadIdx.x;
@@ -309,14 +312,27 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   if (nc == 0) c0 = tile.first;   // for addresses that are not used
   // dt of a vector: a vector, one head's, several heads'
   const int mode = kFast ? (kTied ? 1 : 0) : 2;
-  float head_D[kSV], head_bias[kSV], head_rate[kSV];
-#pragma unroll
-  for (int i = 0; i < kSV; ++i) {
-    const int hd = i < nc ? (c0 + i) / P : 0;
-    head_D[i] = a.D && i < nc ? a.D[hd] : 0.0f;
-    head_bias[i] = a.dt_bias && i < nc ? a.dt_bias[hd] : 0.0f;
-    head_rate[i] = kTied && i < nc ? decay_rate(a.A[hd]) : 0.0f;
+  // of every channel: D, dt_bias and the tied rate, in LDS (a thread's own in registers cost it a wave per SIMD)
+  for (int i = tid; i < kCh; i += kThreads) {
+    const int c = tile.first + i;
+    const bool in = c < tile.end;
+    const int hd = in ? c / P : 0;
+    s_head[0][i] = in && a.D ? a.D[hd] : 0.0f;
+    s_head[1][i] = in && a.dt_bias ? a.dt_bias[hd] : 0.0f;
+    if constexpr (kTied) s_head[2][i] = in ? decay_rate(a.A[hd]) : 0.0f;
   }
+  const int lc = c0 - tile.first;   // of this thread's vector in LDS
+  auto of_heads = [&](int what, float (&v)[kSV]) {
+    if (kFast && lc % kSV == 0) {
+      __builtin_memcpy(v, __builtin_assume_aligned(&s_head[what][lc], kSV > 2 ? 16 : 8), sizeof(v));
+    } else {
+#pragma unroll
+      for (int i = 0; i < kSV; ++i) {
+        const bool in = lc + i >= 0 && (kFast || i < nc);
+        v[i] = in ? s_head[what][in ? lc + i : 0] : 0.0f;
+      }
+    }
+  };
   const int es = dtype == 0 ? 4 : 2, ds = dt_dtype == 0 ? 4 : 2;
   auto column = [](const void* base, Rows r, int64_t batch, int64_t col, int size) {
     return static_cast<const char*>(base) + (batch * r.batch + col) * size;
@@ -382,7 +398,6 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   }
   __syncthreads();
 
-  const int lc = c0 - tile.first;   // of this thread's vector in LDS
   // A tile's y is stored behind the next tile's loads: loads and stores count down in one order, and the
   // wait for the loads, had it the store before it, would be for that too.
   float done[kSV] = {};
@@ -404,32 +419,35 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
   float decay = kTied ? 1.0f : 0.0f;   // of the span (kStates)
   fetch(t_begin);
   for (int64_t t0 = t_begin; t0 < t_end; t0 += kTile) {
-    float u[kSV], z[kSV];
+    Raw<kSV> ku, kz;
     const bool valid = t0 + st < t_last;
     // every load of this tile; said here, where every lane comes by, it spares the waits that the compiler
     // puts before the next requests on behalf of lanes that skip what follows
     __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
     if (nc > 0) {
       float dl[kSV], ml[kSV];
+      float u[kSV];
       as_floats(ru, dtype, u);
-      if (!kStates && a.z) as_floats(rz, dtype, z);
+      ku = ru, kz = rz;
       if (mode == 0) {
         as_floats(rdt, dt_dtype, dl);
       } else {
 #pragma unroll
         for (int i = 0; i < kSV; ++i) dl[i] = as_float(rdt.w[mode == 1 ? 0 : i], dt_dtype);
       }
+      of_heads(1, ml);
 #pragma unroll
-      for (int i = 0; i < kSV; ++i) dl[i] += head_bias[i];
+      for (int i = 0; i < kSV; ++i) dl[i] += ml[i];
       if (a.dt_softplus)
 #pragma unroll
         for (int i = 0; i < kSV; ++i) dl[i] = softplus_fast(dl[i]);
       if (!valid)
 #pragma unroll
         for (int i = 0; i < kSV; ++i) dl[i] = 0.0f, u[i] = 0.0f;
+      if constexpr (kTied) of_heads(2, ml);
 #pragma unroll
       for (int i = 0; i < kSV; ++i) {
-        const float m = kTied ? __builtin_amdgcn_exp2f(dl[i] * head_rate[i]) : dl[i];
+        const float m = kTied ? __builtin_amdgcn_exp2f(dl[i] * ml[i]) : dl[i];
         dl[i] *= u[i];
         ml[i] = m;
       }
@@ -534,10 +552,18 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(Args p) {
           }
         }
 #pragma unroll
-        for (int i = 0; i < kSV; ++i) done[i] = __builtin_fmaf(head_D[i], u[i], sum[i]);
-        if (a.z)
+        for (int i = 0; i < kSV; ++i) done[i] = sum[i];
+        // u and z once more: as they lie in memory they take half the registers meanwhile
+        float v[kSV], skip[kSV];
+        as_floats(ku, dtype, v);
+        of_heads(0, skip);
 #pragma unroll
-          for (int i = 0; i < kSV; ++i) done[i] *= silu(z[i]);
+        for (int i = 0; i < kSV; ++i) done[i] = __builtin_fmaf(skip[i], v[i], done[i]);
+        if (a.z) {
+          as_floats(kz, dtype, v);
+#pragma unroll
+          for (int i = 0; i < kSV; ++i) done[i] *= silu(v[i]);
+        }
         if (!valid)
 #pragma unroll
           for (int i = 0; i < kSV; ++i) done[i] = 0.0f;
