@@ -127,19 +127,22 @@ __device__ __forceinline__ void finish_vec(const LinearArgs& a, int64_t m, int64
 // The exchange of chunks in LDS row r (see above).
 __device__ __forceinline__ int slot_key(int r) { return (r >> 1) & 7; }
 
-// kWM x kWN waves, each a (kBM / kWM) x (kBN / kWN) part of the tile.
-template <typename K, int kBM, int kBN, int kWM, int kWN>
-__global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int mtiles, int ntiles) {
-  constexpr int kThreads = 64 * kWM * kWN;
+// kWM x kWN waves, each a (kBM / kWM) x (kBN / kWN) part of the tile; kSplit such sets of waves share k, each
+// with buffers of its own, and the first adds up the others' sums.
+template <typename K, int kBM, int kBN, int kWM, int kWN, int kSplit>
+__global__ __launch_bounds__(64 * kWM * kWN * kSplit) void linear_tile(LinearArgs a, int mtiles, int ntiles) {
+  constexpr int kThreads = 64 * kWM * kWN;   // of a set
   constexpr int kTM = kBM / kWM / 32, kTN = kBN / kWN / 32;
   constexpr int kBuf = (kBM + kBN) * kLine;
   constexpr int kOutRow = kTN * 32 + 4;   // floats of an LDS row on the way out
-  __shared__ __attribute__((aligned(16))) char lds[2 * kBuf];
+  __shared__ __attribute__((aligned(16))) char all_lds[kSplit * 2 * kBuf];
   static_assert(32 * kOutRow * 4 * kWM * kWN <= 2 * kBuf, "the way out fits");
   typedef typename K::T T;
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int set = kSplit > 1 ? threadIdx.x / kThreads : 0;
+  const int tid = kSplit > 1 ? threadIdx.x % kThreads : threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave / kWN, wn = wave % kWN;
+  char* lds = all_lds + set * 2 * kBuf;
   // tiles of one XCD lie together: bands of four rows of tiles, column by column
   const int id = xcd_remap(blockIdx.x, mtiles * ntiles);
   constexpr int kBand = 4;
@@ -149,7 +152,11 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
   const int64_t n0 = (int64_t)(in / rows) * kBN;
 
   const int64_t kbytes = a.k * (int64_t)sizeof(T);
-  const int whole = (int)(kbytes / kLine), ktiles = (int)((kbytes + kLine - 1) / kLine);
+  // the k-tiles of this set: as many for every set (they meet at the same barriers), zeros behind the last
+  const int all = (int)((kbytes + kLine - 1) / kLine), ktiles = (all + kSplit - 1) / kSplit;
+  const int64_t k0 = (int64_t)set * ktiles * kLine;
+  int whole = (int)((kbytes - k0) / kLine);
+  whole = kbytes < k0 ? 0 : (whole < ktiles ? whole : ktiles);
   // this thread's part of a k-tile: slot tid % kChunks of LDS row r = i * kThreads / kChunks + tid / kChunks
   // holds chunk slot ^ key(r) of that row
   constexpr int kLoadRows = kThreads / kChunks;
@@ -166,8 +173,8 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
     r = r < left ? r : left - 1;
     offset[i] = (uint32_t)(r * (i < kA ? a.x_row : a.w_row) * (int64_t)sizeof(T)) + chunk * 16;
   }
-  const char* xp = static_cast<const char*>(a.x) + m0 * a.x_row * (int64_t)sizeof(T);
-  const char* wp = static_cast<const char*>(a.w) + n0 * a.w_row * (int64_t)sizeof(T);
+  const char* xp = static_cast<const char*>(a.x) + m0 * a.x_row * (int64_t)sizeof(T) + k0;
+  const char* wp = static_cast<const char*>(a.w) + n0 * a.w_row * (int64_t)sizeof(T) + k0;
 
   typename K::Acc32 acc[kTN][kTM] = {};
   const int fr = lane & 31, fk = lane >> 5;
@@ -191,7 +198,7 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
   auto request = [&](int kt, int i, auto inside) {   // inside: a whole k-tile
     const char* p = (i < kA ? xp : wp) + (int64_t)kt * kLine + offset[i];
     if constexpr (decltype(inside)::value) __builtin_memcpy(&part[i], p, 16);
-    else part[i] = load_chunk<T>(p, 0, kbytes - (int64_t)kt * kLine - chunk * 16);
+    else part[i] = load_chunk<T>(p, 0, kbytes - k0 - (int64_t)kt * kLine - chunk * 16);
   };
   auto put = [&](int kt, int i) {
     char* buf = lds + (kt & 1) * kBuf + (i < kA ? 0 : kBM * kLine) + tid * 16;
@@ -254,6 +261,38 @@ __global__ __launch_bounds__(64 * kWM * kWN) void linear_tile(LinearArgs a, int 
   }
   for (; kt < ktiles; ++kt) k_tile(kt, std::false_type());
   __syncthreads();
+  if constexpr (kSplit > 1) {
+    typedef std::conditional_t<std::is_same_v<K, I8>, int4, float4> Four;
+    static_assert(kThreads * kTN * kTM * 64 <= 2 * kBuf, "a set's sums fit its buffers");
+    auto place = [&](char* at, int j, int i, int q) {
+      return reinterpret_cast<Four*>(at) + ((((j * kTM + i) * 4 + q) * (kThreads / 64) + wave) * 64 + lane);
+    };
+    if (set > 0) {
+#pragma unroll
+      for (int j = 0; j < kTN; ++j)
+#pragma unroll
+        for (int i = 0; i < kTM; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            Four v;
+            v.x = acc[j][i][4 * q], v.y = acc[j][i][4 * q + 1], v.z = acc[j][i][4 * q + 2], v.w = acc[j][i][4 * q + 3];
+            *place(lds, j, i, q) = v;
+          }
+    }
+    __syncthreads();
+    if (set > 0) return;
+    for (int k = 1; k < kSplit; ++k)
+#pragma unroll
+      for (int j = 0; j < kTN; ++j)
+#pragma unroll
+        for (int i = 0; i < kTM; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const Four v = *place(all_lds + k * 2 * kBuf, j, i, q);
+            acc[j][i][4 * q] += v.x, acc[j][i][4 * q + 1] += v.y;
+            acc[j][i][4 * q + 2] += v.z, acc[j][i][4 * q + 3] += v.w;
+          }
+  }
 
   // a lane holds row fr of the 32 x 32 block, columns 8 q + 4 fk + (0..3); on the way out it has eight
   // columns, the same ones of every row
@@ -395,11 +434,11 @@ __global__ __launch_bounds__(64 * kWaves) void linear_rows(LinearArgs a) {
   }
 }
 
-template <typename K, int kBM, int kBN, int kWM, int kWN>
+template <typename K, int kBM, int kBN, int kWM, int kWN, int kSplit = 1>
 hipError_t run_tile(const LinearArgs& a, hipStream_t st) {
   const int64_t mt = (a.m + kBM - 1) / kBM, nt = (a.n + kBN - 1) / kBN;
-  linear_tile<K, kBM, kBN, kWM, kWN>
-      <<<dim3((unsigned)(mt * nt)), 64 * kWM * kWN, 0, st>>>(a, (int)mt, (int)nt);
+  linear_tile<K, kBM, kBN, kWM, kWN, kSplit>
+      <<<dim3((unsigned)(mt * nt)), 64 * kWM * kWN * kSplit, 0, st>>>(a, (int)mt, (int)nt);
   return hipGetLastError();
 }
 
@@ -423,9 +462,9 @@ template <typename K> hipError_t run(const LinearArgs& a, hipStream_t st) {
   // 256 x 128, 1108 with 128 x 128, 1700 with 64 x 64.  Where another than the largest wins: 16384 x 768 x
   // 1536 49.7 / 47.2 us with 256 x 192, 2048 x 2560 x 5120 104 / 68.7 with 256 x 128, 512 x 5120 x 2560
   // 55.4 / 24.0 with 128 x 128, 128 x 5120 x 2560 54.2 / 16.5 with 64 x 64.
+  auto count = [&](int64_t bm, int64_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
   auto cost = [&](int64_t bm, int64_t bn, double rate) {
-    const int64_t tiles = ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn);
-    return (double)((tiles + 255) / 256) * (double)(bm * bn) / rate;
+    return (double)((count(bm, bn) + 255) / 256) * (double)(bm * bn) / rate;
   };
   const double costs[] = {cost(256, 256, 1.0), cost(256, 192, 0.9), cost(256, 128, 0.87),
                           cost(128, 128, 0.81), cost(64, 64, 0.53)};
@@ -437,8 +476,13 @@ template <typename K> hipError_t run(const LinearArgs& a, hipStream_t st) {
     case 1: return run_tile<K, 256, 192, 4, 2>(a, st);
     case 2: return run_tile<K, 256, 128, 4, 2>(a, st);
     case 3: return run_tile<K, 128, 128, 2, 2>(a, st);
-    default: return run_tile<K, 64, 64, 2, 2>(a, st);
+    default: break;
   }
+  // Small tiles that leave CUs without a second one, over a long k: four sets of waves share it (128 x 5120 x
+  // 2560 fp16 16.3 -> 12.3 us, 200 x 2000 x 2000 12.1 -> 10.5, 100 x 768 x 1536 8.8 -> 7.8; over a short one their
+  // ends cost more: 300 x 1111 x 1600 int8 8.7 -> 13.2).
+  const bool split = count(64, 64) <= 256 && a.k * (int64_t)sizeof(typename K::T) >= 24 * kLine;
+  return split ? run_tile<K, 64, 64, 2, 2, 4>(a, st) : run_tile<K, 64, 64, 2, 2>(a, st);
 }
 
 }  // namespace

@@ -304,11 +304,13 @@ def test_linear(ssdi8, M, O, K, dtype, bias, act, res, y32, before):
     R.assert_within(got, y, R.rounded(yd, y, e), "y")
 
 
-@pytest.mark.parametrize("M,O", [(4090, 4090), (4090, 3060), (4090, 2040), (2040, 2040), (1000, 1000)])
-@pytest.mark.parametrize("K,dtype", [(80, F16), (321, "i8")])
+@pytest.mark.parametrize("M,O", [(4090, 4090), (4090, 3060), (4090, 2040), (2040, 2040), (300, 16500),
+                                 (1000, 1000), (640, 1920), (65, 70)])
+@pytest.mark.parametrize("K,dtype", [(80, F16), (321, "i8"), (1611, BF16)])
 def test_linear_tiles(ssdi8, M, O, K, dtype):
-    """A size for each tile of the larger products (256 x 256, 192, 128, 128 x 128, 64 x 64), whole value
-    by whole value: small integers, whose products and sums every type holds exactly."""
+    """A size for each tile of the larger products (256 x 256, 192, 128, 128 x 128, 64 x 64, the last two
+    with k split over sets of waves too), whole value by whole value: small integers, whose products and
+    sums every type holds exactly."""
     r = Draw(M + O)
     x, w = (r.uniform(-2.5, 2.5, *s).round() for s in ((M, K), (O, K)))
     b, rr = r.uniform(-9, 9, O).round(), r.uniform(-9, 9, M, O).round()
