@@ -26,7 +26,7 @@ ssdi8_status check_conv(int64_t batch, int64_t seqlen, int64_t channels, const s
                         bool step, ssdi8::ConvOut* out) {
   if (bad_size(batch, 0) || bad_size(seqlen, 0) || bad_size(channels, 1)) return SSDI8_ERR_SHAPE;
   if (channels > kMaxSize - 4096 || (double)batch * (seqlen + 64) * channels > kMaxCount ||
-      (double)batch * (seqlen / 64 + 1) * (channels / 512 + 1) > kMaxGrid)
+      (double)batch * (seqlen / 32 + 1) * (channels / 512 + 2) > kMaxGrid)
     return SSDI8_ERR_SHAPE;
   if (!a) return SSDI8_ERR_NULL;
   if (!is_float(a->dtype)) return SSDI8_ERR_ARG;

@@ -7,17 +7,17 @@
 // channels, its weights and the last W-1 rows in registers and walks kTokens tokens, so a row is read
 // once except for the W-1 rows in front of each walk (from the L2 cache).  64 lanes lie along the
 // channels: 1 KB of a row per access.  4 x 4096 x 5376 fp16, columns of rows twice as wide into three
-// outputs: 86 us, 4.1 TB/s (a copy of the same rows 64); 32 tokens per walk, 16 took 89.  A token of 8
+// outputs: 78 us, 4.5 TB/s (a copy of the same rows 64).  A token of 8
 // sequences: 4 us, a launch and one chain of loads.
 #include <type_traits>
 
 #include "block.hpp"
+#include "common.hpp"
 
 namespace ssdi8 {
 
 namespace {
 
-constexpr int kTokens = 32;   // of one thread's walk
 constexpr int kWaves = 4;     // walks of a workgroup, one behind the other
 
 // A thread's channels: vector `vec` of the columns, which never lies in two outputs.  The last vector of an
@@ -97,13 +97,15 @@ __device__ __forceinline__ int64_t length_of(const int* lengths, int64_t b, int6
   return lengths[b] < 0 ? 0 : (lengths[b] < L ? lengths[b] : L);
 }
 
-template <typename T, int W, bool kSilu>
+template <typename T, int W, bool kSilu, int kTokens>
 __global__ __launch_bounds__(64 * kWaves) void conv_kernel(
     const T* __restrict__ x, Rows xr, const float* __restrict__ w, const float* __restrict__ bias,
     const T* __restrict__ init, const int* __restrict__ lengths, ConvOut out, T* __restrict__ final_state,
     int64_t L, int D, int nctile, int64_t nttile) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t bid = blockIdx.x;
+  // Short walks behind one another on one XCD: the rows that they share come from its L2 (3 x 5000 x 1793 fp16
+  // 26.1 -> 23.7 us).  The longest share too little for it, and 65536 x 1024 fp32 went from 116 to 141 us.
+  const int64_t bid = kTokens < 64 ? xcd_remap(blockIdx.x, gridDim.x) : (int)blockIdx.x;
   const int ct = (int)(bid % nctile);
   const int64_t tt = (bid / nctile) % nttile;
   const int64_t b = bid / nctile / nttile;
@@ -264,16 +266,29 @@ hipError_t launch_conv(int dtype, int width, int64_t batch, int64_t seqlen, int6
                        hipStream_t st) {
   ConvOut out = outputs;
   const int nctile = count_vectors(out);
-  int64_t nttile = (seqlen + kTokens * kWaves - 1) / (kTokens * kWaves);
-  if (nttile == 0) nttile = 1;   // no tokens: the states alone
+  // Tokens of a walk: 64 where that leaves every CU two workgroups (4 x 4096 x 5376 fp16: 78 us, 86 with 32, 89
+  // with 16), 32 where that leaves it one, else 8 (2048 x 1792: 8.7 us, 14.2 with 32).
+  auto count = [&](int64_t tokens) {
+    const int64_t n = (seqlen + tokens * kWaves - 1) / (tokens * kWaves);
+    return n > 0 ? n : 1;   // no tokens: the states alone
+  };
+  const int64_t lines = nctile * batch;
+  const int tokens = lines * count(64) >= 512 ? 64 : lines * count(32) >= 256 ? 32 : 8;
+  const int64_t nttile = count(tokens);
   const int64_t grid = nctile * nttile * batch;
   return for_type(dtype, width, silu, [&](auto t, auto w, auto s) {
     using T = decltype(t);
     constexpr int W = decltype(w)::value;
     const bool over = final_state && final_state == init;
-    conv_kernel<T, W, decltype(s)::value><<<dim3((unsigned)grid), 64 * kWaves, 0, st>>>(
-        static_cast<const T*>(x), xr, weight, bias, static_cast<const T*>(init), lengths, out,
-        over ? nullptr : static_cast<T*>(final_state), seqlen, (int)channels, nctile, nttile);
+    auto go = [&](auto tokens) {
+      conv_kernel<T, W, decltype(s)::value, decltype(tokens)::value>
+          <<<dim3((unsigned)grid), 64 * kWaves, 0, st>>>(
+              static_cast<const T*>(x), xr, weight, bias, static_cast<const T*>(init), lengths, out,
+              over ? nullptr : static_cast<T*>(final_state), seqlen, (int)channels, nctile, nttile);
+    };
+    if (tokens == 64) go(std::integral_constant<int, 64>());
+    else if (tokens == 32) go(std::integral_constant<int, 32>());
+    else go(std::integral_constant<int, 8>());
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || !over) return e;
     conv_final_kernel<T, W><<<dim3((unsigned)(nctile * batch)), 64, 0, st>>>(

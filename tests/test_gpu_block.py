@@ -97,6 +97,26 @@ def test_conv_token_by_token(ssdi8, B, D, W, dtype, split):
     assert torch.equal(state.double().cpu(), last)
 
 
+@pytest.mark.parametrize("B,L,D,W,split,lengths", [(2, 70, 1540, 4, (1029, 260, 251), [70, 1]),
+                                                   (3, 5, 20, 3, None, [0, 2, 1]), (1, 0, 9, 4, None, None)])
+def test_conv_state_in_place(ssdi8, B, L, D, W, split, lengths):
+    """The state of a resumed sequence may be its own final state."""
+    import ctypes
+    r = Draw(D)
+    x, w, s0 = r.normal(B, L, D, dtype=F16), r.uniform(-0.7, 0.7, D, W), r.normal(B, W - 1, D, dtype=F16)
+    n = torch.tensor(lengths, dtype=torch.int32) if lengths else None
+    y, e, last = R.conv(x.double(), w, None, "silu", s0.double(), n)
+    xd, wd, st, nd = dev(x), dev(w), dev(s0), dev(n)
+    a, out = ssdi8._conv(xd, wd, None, "silu", split, None, B, L, None)
+    a.x_token_stride = xd.stride(1)
+    a.init_state = a.final_state = st.data_ptr()
+    a.lengths = nd.data_ptr() if n is not None else None
+    stream = torch.cuda.current_stream().cuda_stream
+    assert ssdi8.lib().ssdi8_causal_conv(B, L, D, ctypes.byref(a), stream) == ssdi8.OK
+    R.assert_within(torch.cat(out, -1), y, R.rounded(F16, y, e), "y")
+    assert torch.equal(st.double().cpu(), last)
+
+
 # ------------------------------------------------------------------------------ selective scan
 SCAN = [  # B, L, heads, headdim, groups, N, tied, dtype, dt fp32, z, init, lengths, columns before
     (1, 1, 64, 1, 1, 16, False, F16, False, True, False, None, 0),
