@@ -397,7 +397,8 @@ ssdi8_status ssdi8_causal_conv_step(int64_t batch, int64_t channels, const ssdi8
  * headdim 1 with A [D,N] is the form with a time step and decays per channel; tied with headdim 64
  * and N = 128 is the SSD layer's recurrence, for lengths that are no multiple of its chunk (its fp32
  * final states are this call's initial states and the other way round).  Any seqlen; dstate up to
- * 256; D a multiple of ngroups.  init_state and final_state may be the same memory.
+ * 256; D a multiple of ngroups.  init_state and final_state may be the same memory.  With seqlen = 0
+ * u, dt, B, C and y may be NULL; A may not where a final state is wanted.
  */
 typedef struct {
   int dtype;                          /* of u, B, C, z and y                                      */

@@ -83,7 +83,9 @@ ssdi8_status check_scan(const ssdi8_sel_scan_dims* d, const ssdi8_sel_scan_args*
   for (int i = 0; i < 5; ++i)
     if (bad_stride(strides[i]) || (!step && bad_stride(tokens[i]))) return SSDI8_ERR_SHAPE;
   const bool work = d->batch > 0 && (step || d->seqlen > 0);
-  if (work && (!a->u || !a->dt || !a->A || !a->B || !a->C || !a->y)) return SSDI8_ERR_NULL;
+  if (work && (!a->u || !a->dt || !a->B || !a->C || !a->y)) return SSDI8_ERR_NULL;
+  // the rates are read before the tokens are counted: by the launch that only copies the state, too
+  if ((work || (d->batch > 0 && a->final_state)) && !a->A) return SSDI8_ERR_NULL;
   if (work && step && !a->final_state) return SSDI8_ERR_NULL;
   const uintptr_t es = size_of(a->dtype);
   if (off(a->u, es) || off(a->dt, size_of(a->dt_dtype)) || off(a->B, es) || off(a->C, es) ||

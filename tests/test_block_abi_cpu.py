@@ -115,6 +115,21 @@ def test_selective_scan(ssdi8):
     assert s.selective_scan_workspace_size(s.SelScanDims(**{**sizes, "seqlen": 1})) == 0
 
 
+def test_selective_scan_of_no_tokens(ssdi8):
+    """The final state of no tokens is a launch like any other, which reads A: refused without it, while
+    what belongs to tokens may be missing."""
+    s, L = ssdi8, ssdi8.lib()
+    for tied in (0, 1):
+        d = s.SelScanDims(batch=2, seqlen=0, nheads=16, headdim=4, ngroups=2, dstate=16)
+        a = s.SelScanArgs(dtype=s.F16, dt_dtype=s.F32, tied=tied, final_state=A16)
+        call = lambda: L.ssdi8_selective_scan(ctypes.byref(d), ctypes.byref(a), None)
+        assert call() == s.ERR_NULL
+        a.final_state = None
+        assert call() == s.OK      # nothing is done
+        d.batch, a.final_state = 0, A16
+        assert call() == s.OK
+
+
 def test_gated_norm(ssdi8):
     s, L = ssdi8, ssdi8.lib()
     a = s.NormArgs(dtype=s.F16, x=A16, x_row_stride=16, z=A16, z_row_stride=16, residual=A16, weight=A16,
