@@ -86,7 +86,7 @@ class Mamba2Block:
                 init_state=None if state is None else state.view(B, self.H, -1, ssdi8.N_DIM))
             y[:, :whole] = head["y"].view(B, whole, self.di)
             state = head["final_state"].view(B, self.di, ssdi8.N_DIM)
-        if whole < L:
+        if whole < L or not L:   # no tokens: the scan copies the cache's state, or gives zeros
             rest = lambda t: t[:, whole:]
             tail = ssdi8.selective_scan(rest(u), rest(dt), self.w["A"], self._groups(rest(Bt)),
                                         self._groups(rest(Ct)), D=self.w["D"], init_state=state)

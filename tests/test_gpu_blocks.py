@@ -114,3 +114,44 @@ def test_mamba_block(blocks, int8):
         assert off(y[b:b + 1, :k], want[:, :k]) < tol
         assert off(nxt[b:b + 1], want[:, k]) < tol
         assert off(cache["state"][b:b + 1], s) < tol
+
+
+def mamba(seed, d=96, di=160, N=16, rank=8):
+    g = torch.Generator().manual_seed(seed)
+    n = lambda *s, scale=1.0: scale * torch.randn(*s, generator=g)
+    return {"norm": 1 + n(d, scale=0.1), "in_proj": n(2 * di, d, scale=d ** -0.5).half(),
+            "conv": n(di, 4, scale=0.4), "conv_bias": n(di, scale=0.1),
+            "x_proj": n(rank + 2 * N, di, scale=2 * di ** -0.5).half(),
+            "dt_proj": n(di, rank, scale=0.3 * rank ** -0.5).half(), "dt_bias": n(di, scale=0.3) - 2,
+            "A": -torch.exp(2.7 * torch.rand(di, N, generator=g)), "D": 1 + n(di, scale=0.1),
+            "out_proj": n(d, di, scale=di ** -0.5).half()}
+
+
+def no_tokens(blocks, kind, int8):
+    """No tokens leave the cache's values, in memory of their own, or zeros; tokens go on from there."""
+    if kind == "mamba2":
+        w, sizes = mamba2(11)
+        block, d = blocks.Mamba2Block(cuda(w), int8=int8, **sizes), 192
+    else:
+        block, d = blocks.MambaBlock(cuda(mamba(11)), int8=int8), 96
+    x = torch.randn(2, 9, d, generator=torch.Generator().manual_seed(3)).half().cuda()
+    none = x[:, :0]
+    y, fresh = block.prefill(none)
+    assert y.shape == none.shape and y.dtype == x.dtype
+    assert not fresh["conv"].any() and not fresh["state"].any()
+    # the first token on the empty cache is a prompt of one token
+    got = block.step(x[:, 0], fresh)
+    want, one = block.prefill(x[:, :1])
+    assert off(got, want[:, 0]) < TOL and off(fresh["state"], one["state"]) < TOL
+    # on a cache: its values, which a step on the new one leaves alone
+    _, cache = block.prefill(x[:, :8].contiguous())
+    held = {k: v.clone() for k, v in cache.items()}
+    y, same = block.prefill(none, cache)
+    assert y.shape == none.shape and all(torch.equal(same[k], held[k]) for k in held)
+    block.step(x[:, 8], same)
+    assert all(torch.equal(cache[k], held[k]) for k in held)
+
+
+@pytest.mark.parametrize("kind", ["mamba2", "mamba"])
+def test_prompt_of_no_tokens(blocks, kind):
+    no_tokens(blocks, kind, False)
