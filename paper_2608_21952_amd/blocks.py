@@ -36,6 +36,8 @@ class Projection:
     @staticmethod
     def quantize(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
         rows = x.reshape(-1, 1, 1, x.shape[-1])
+        if not rows.numel():   # the quantizer takes no NULL steps, and no rows have none
+            return x.to(torch.int8), torch.empty(0, dtype=torch.float32, device=x.device)
         codes, steps = ssdi8.quantize_act(rows, "token")
         return codes.view(x.shape), steps
 

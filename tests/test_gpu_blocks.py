@@ -155,3 +155,8 @@ def no_tokens(blocks, kind, int8):
 @pytest.mark.parametrize("kind", ["mamba2", "mamba"])
 def test_prompt_of_no_tokens(blocks, kind):
     no_tokens(blocks, kind, False)
+
+
+@pytest.mark.parametrize("kind", ["mamba2", "mamba"])
+def test_prompt_of_no_tokens_int8(blocks, kind):
+    no_tokens(blocks, kind, True)
