@@ -48,11 +48,16 @@ class Mamba2Block:
     scan from the state that they leave; both keep the state in fp32.
 
     weights: norm (d), in_proj (2 di + 2 G N, d) for z, x, B, C, dt_proj (H, d), dt_bias (H),
-    conv (di + 2 G N, W), conv_bias, A (H), D (H), gate_norm (di), out_proj (d, di); di = H * 64."""
+    conv (di + 2 G N, W), conv_bias, A (H), D (H), gate_norm (di), out_proj (d, di); di = H * 64.
+    gate_groups: equal groups of channels that the norm behind the scan takes each by itself; 1, over all
+    channels, unless said (models with several groups of B and C often have as many here)."""
 
     def __init__(self, weights: Dict[str, torch.Tensor], *, nheads: int, ngroups: int,
-                 int8: bool = False, eps: float = 1e-5):
+                 gate_groups: int = 1, int8: bool = False, eps: float = 1e-5):
         self.w, self.H, self.G, self.eps = weights, nheads, ngroups, eps
+        if gate_groups < 1 or nheads * ssdi8.P_DIM % gate_groups:
+            raise ValueError(f"gate_groups must divide the {nheads * ssdi8.P_DIM} channels, got {gate_groups}")
+        self.gate_groups = gate_groups
         self.di, self.gn = nheads * ssdi8.P_DIM, ngroups * ssdi8.N_DIM
         self.in_proj = Projection(weights["in_proj"], int8)
         self.out_proj = Projection(weights["out_proj"], int8)
@@ -64,7 +69,8 @@ class Mamba2Block:
         return zx[..., :self.di], zx[..., self.di:], dt
 
     def _back(self, y, z, x):
-        y = ssdi8.gated_norm(y, self.w["gate_norm"], z=z, eps=self.eps)["y"]
+        y = ssdi8.gated_norm(y, self.w["gate_norm"], z=z, eps=self.eps,
+                             groups=self.gate_groups)["y"]
         return self.out_proj(y, residual=x)
 
     def _groups(self, t):

@@ -160,3 +160,39 @@ def test_prompt_of_no_tokens(blocks, kind):
 @pytest.mark.parametrize("kind", ["mamba2", "mamba"])
 def test_prompt_of_no_tokens_int8(blocks, kind):
     no_tokens(blocks, kind, True)
+
+
+@pytest.mark.parametrize("gate_groups", [2, 4])
+def test_mamba2_block_with_a_grouped_gate_norm(blocks, gate_groups):
+    """The norm behind the scan over groups of channels, as layers with several groups of B and C have it:
+    prompt, tokens, and the 64-bit block with the same groups."""
+    L, H, G = 260, 4, 2
+    w, sizes = mamba2(7, H=H, G=G)
+    block = blocks.Mamba2Block(cuda(w), gate_groups=gate_groups, **sizes)
+    x = torch.randn(2, L + 1, 192, generator=torch.Generator().manual_seed(2)).half()
+    want, _, state = mamba2_64_grouped(w, x.double(), H, G, gate_groups)
+    y, cache = block.prefill(x[:, :L].cuda())
+    assert off(y, want[:, :L]) < TOL
+    assert off(block.step(x[:, L].cuda(), cache), want[:, L]) < TOL
+    assert off(cache["state"], state) < TOL
+    # without the option the norm is over all channels, as ever
+    plain, _, _ = mamba2_64(w, x.double(), H, G)
+    assert off(blocks.Mamba2Block(cuda(w), **sizes).prefill(x[:, :L].cuda())[0], plain[:, :L]) < TOL
+    assert off(plain, want) > 2 * TOL   # the two are told apart
+    with pytest.raises(ValueError, match="gate_groups"):
+        blocks.Mamba2Block(cuda(w), gate_groups=3, **sizes)
+
+
+def mamba2_64_grouped(w, x, H, G, groups):
+    d64 = {k: v.double() for k, v in w.items()}
+    B, L, _ = x.shape
+    di, gn = 64 * H, 128 * G
+    rows = lambda v: v.reshape(B * L, -1)
+    h = R.norm(rows(x), d64["norm"], None, None, 1e-5, 1, False)[0].view(B, L, -1)
+    zx = h @ d64["in_proj"].t()
+    c, _, conv = R.conv(zx[..., di:], w["conv"], w["conv_bias"], "silu", None, None)
+    u, Bt, Ct = c.split((di, gn, gn), -1)
+    y, _, state, _ = R.scan(u, h @ d64["dt_proj"].t() + d64["dt_bias"], d64["A"], Bt.view(B, L, G, 128),
+                            Ct.view(B, L, G, 128), d64["D"], None, None, True, None, None)
+    y = R.norm(rows(y), d64["gate_norm"], rows(zx[..., :di]), None, 1e-5, groups, False)[0].view(B, L, di)
+    return x + y @ d64["out_proj"].t(), conv, state
