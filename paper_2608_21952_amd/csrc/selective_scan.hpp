@@ -296,8 +296,13 @@ __global__ __launch_bounds__(kThreads, kS == 2 && kFast ? 3 : 1) void scan_kerne
         for (int k = 0; k < kAhead; ++k)
           if (c + k < span)
 #pragma unroll
-            for (int i = 0; i < kS; ++i)
-              h[i] = __builtin_fmaf(kTied ? dec[k] : __builtin_amdgcn_exp2f(dec[k] * rate[i]), h[i], end[k][i]);
+            for (int i = 0; i < kS; ++i) {
+              const float f = kTied ? dec[k] : __builtin_amdgcn_exp2f(dec[k] * rate[i]);
+              // a span's decay may be below the normal range, where none of its tokens' is: an infinite state stays
+              // one, as it does token by token
+              const bool stays = f == 0.0f && __builtin_fabsf(h[i]) == __builtin_inff();
+              h[i] = __builtin_fmaf(stays ? 1.0f : f, h[i], end[k][i]);
+            }
       }
     }
   }
