@@ -1,10 +1,12 @@
 """The operators around the SSD layer where their forms differ, against the 64-bit forms and bounds of
 block_ref.py."""
+import ctypes
+
 import pytest
 import torch
 
 import block_ref as R
-from test_gpu_block import BF16, F16, F32, Draw, dev, scan_ref
+from test_gpu_block import BF16, F16, F32, Draw, cut, dev, scan_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -14,6 +16,51 @@ def ssdi8():
     from paper_2608_21952_amd import ssdi8 as s
     s.lib()
     return s
+
+
+# ------------------------------------------------------------------------------ convolution
+# B waves lie along the channels here: 256 of them with two workgroups each take walks of 32 tokens, 512
+# take walks of 64
+WALKS = [(256, 130, 8, 4, F16, None, 0), (256, 130, 21, 3, BF16, (9, 8, 4), 5),
+         (512, 70, 8, 4, F16, None, 3), (512, 300, 19, 4, F32, (1, 10, 8), 0),
+         (512, 257, 24, 2, BF16, (8, 16), 8)]
+
+
+def walk_inputs(B, L, D, W, dtype):
+    r = Draw(B + L + D)
+    x, w, s0 = r.normal(B, L, D, dtype=dtype), r.uniform(-0.7, 0.7, D, W), r.normal(B, W - 1, D, dtype=dtype)
+    n = torch.tensor([(L, 0, 1, L - 1, 64, 65, 32, 3)[b % 8] for b in range(B)], dtype=torch.int32)
+    return x, w, r.normal(D), s0, n
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("B,L,D,W,dtype,split,before", WALKS)
+def test_conv_walks(ssdi8, B, L, D, W, dtype, split, before, ragged):
+    x, w, b, s0, n = walk_inputs(B, L, D, W, dtype)
+    y, e, last = R.conv(x.double(), w, b, "silu", s0.double(), n if ragged else None)
+    xd = x.clone()
+    if ragged:
+        xd[torch.arange(L)[None] >= n[:, None]] = float("nan")
+    out = ssdi8.causal_conv(cut(xd, before), dev(w), bias=dev(b), split=split, init_state=dev(s0),
+                            lengths=dev(n) if ragged else None)
+    got = out["y"] if split is None else torch.cat(out["y"], -1)
+    R.assert_within(got, y, R.rounded(dtype, y, e), "y")
+    assert torch.equal(out["final_state"].double().cpu(), last)
+
+
+def test_conv_walk_with_the_state_in_place(ssdi8):
+    B, L, D, W = 512, 300, 19, 4
+    x, w, b, s0, n = walk_inputs(B, L, D, W, F16)
+    y, e, last = R.conv(x.double(), w, None, "silu", s0.double(), n)
+    xd, wd, st, nd = dev(x), dev(w), dev(s0), dev(n)
+    a, out = ssdi8._conv(xd, wd, None, "silu", None, None, B, L, None)
+    a.x_token_stride = xd.stride(1)
+    a.init_state = a.final_state = st.data_ptr()
+    a.lengths = nd.data_ptr()
+    stream = torch.cuda.current_stream().cuda_stream
+    assert ssdi8.lib().ssdi8_causal_conv(B, L, D, ctypes.byref(a), stream) == ssdi8.OK
+    R.assert_within(out[0], y, R.rounded(F16, y, e), "y")
+    assert torch.equal(st.double().cpu(), last)
 
 
 # ------------------------------------------------------------------------------ selective scan
