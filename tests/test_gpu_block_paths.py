@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import block_ref as R
-from test_gpu_block import BF16, F16, F32, Draw, cut, dev, scan_ref
+from test_gpu_block import BF16, F16, F32, Draw, cut, d64, dev, scan_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -61,6 +61,40 @@ def test_conv_walk_with_the_state_in_place(ssdi8):
     assert ssdi8.lib().ssdi8_causal_conv(B, L, D, ctypes.byref(a), stream) == ssdi8.OK
     R.assert_within(out[0], y, R.rounded(F16, y, e), "y")
     assert torch.equal(st.double().cpu(), last)
+
+
+# ------------------------------------------------------------------------------ gated norm
+# Walks of two rows from 4096 groups of a workgroup or 16384 of a wave each, of four from twice as many
+ROWS = [(8195, 1032, 1, F16, True, True, False), (4099, 1032, 1, BF16, True, False, True),
+        (8197, 1029, 1, F32, False, True, False), (16390, 1000, 1, F16, True, True, True),
+        (33001, 40, 1, F16, True, True, False), (17001, 82, 2, BF16, True, False, False),
+        (33003, 7, 1, F16, True, True, False), (33003, 15, 1, F32, False, False, False)]
+
+
+@pytest.mark.parametrize("M,D,groups,dtype,z,res,before", ROWS)
+def test_norm_walks(ssdi8, M, D, groups, dtype, z, res, before):
+    r = Draw(M + D)
+    x, w = dev(r.normal(M, D, dtype=dtype)), dev(1 + 0.1 * r.normal(D))
+    zz = dev(r.normal(M, D, dtype=dtype, scale=3.0)) if z else None
+    rr = dev(r.normal(M, D, dtype=dtype)) if res else None
+    x[M - 1] = 0
+    y, e, s = R.norm(x.double(), w.double(), d64(zz), d64(rr), 1e-5, groups, before)
+    y, e, s = y.cpu(), e.cpu(), s.cpu()
+    kw = dict(groups=groups, norm_before_gate=before)
+    out = ssdi8.gated_norm(x, w, z=zz, residual=rr, **kw)
+    R.assert_within(out["y"], y, R.rounded(dtype, y, e), "y")
+    if res:
+        R.assert_within(out["residual"], s, R.rounded(dtype, s, R.U * s.abs()), "residual")
+    # columns of wider rows
+    wide = torch.full((M, D + 5), float("nan"), dtype=dtype, device="cuda")
+    wide[:, 3:3 + D] = x
+    again = ssdi8.gated_norm(wide[:, 3:3 + D], w, z=zz, residual=rr, **kw)
+    assert torch.equal(again["y"], out["y"])
+    # y over x, the sum over the residual
+    place = ssdi8.gated_norm(x, w, z=zz, residual=rr, y=x, residual_out=rr, **kw)
+    assert place["y"] is x and torch.equal(x, out["y"])
+    if res:
+        assert place["residual"] is rr and torch.equal(rr, out["residual"])
 
 
 # ------------------------------------------------------------------------------ selective scan
