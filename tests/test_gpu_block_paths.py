@@ -1,5 +1,7 @@
-"""The operators around the SSD layer where their forms differ, against the 64-bit forms and bounds of
-block_ref.py."""
+"""The operators around the SSD layer at the sizes that choose their other forms: the convolution's walks of
+32 and 64 tokens, the norm's walks of two and four rows, the few-row products' unrolled lines and wider
+tiles, int8 sums shared by sets of waves, the selective scan's compile-time forms.  Against the 64-bit
+forms and bounds of block_ref.py, or, for products, whole value by whole value."""
 import ctypes
 
 import pytest
@@ -95,6 +97,26 @@ def test_norm_walks(ssdi8, M, D, groups, dtype, z, res, before):
     assert place["y"] is x and torch.equal(x, out["y"])
     if res:
         assert place["residual"] is rr and torch.equal(rr, out["residual"])
+
+
+# ------------------------------------------------------------------------------ projections
+FEW = [(8, 70, 2600), (16, 4100, 2100), (24, 4100, 300), (32, 4111, 2600), (30, 70, 2600), (50, 100, 2600),
+       (64, 8190, 320), (40, 8200, 330)]
+SPLIT = [(65, 70, 3211), (1000, 1000, 3211), (130, 700, 6500)]
+
+
+@pytest.mark.parametrize("M,O,K", FEW + SPLIT)
+@pytest.mark.parametrize("dtype", [F16, BF16, torch.int8])
+def test_linear_forms(ssdi8, M, O, K, dtype):
+    """Small integers, whose products and sums every type holds exactly."""
+    r = Draw(M + O)
+    x, w = (r.uniform(-2.5, 2.5, *s).round() for s in ((M, K), (O, K)))
+    b, rr = r.uniform(-9, 9, O).round(), r.uniform(-9, 9, M, O).round()
+    kw = dict(x_scale=torch.ones(M, device="cuda"), w_scale=torch.ones(O, device="cuda")) \
+        if dtype == torch.int8 else {}
+    got = ssdi8.linear(x.to(dtype).cuda(), w.to(dtype).cuda(), bias=dev(b), residual=dev(rr), y_dtype=F32, **kw)
+    want = x.cuda().double() @ w.cuda().double().t() + dev(b) + dev(rr)
+    assert torch.equal(got.double(), want)
 
 
 # ------------------------------------------------------------------------------ selective scan
