@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import block_ref as R
-from test_gpu_block import BF16, F16, F32, Draw, cut, d64, dev, scan_ref
+from test_gpu_block import BF16, F16, F32, Draw, cut, d64, dev, scan_inputs, scan_ref
 
 pytestmark = pytest.mark.gpu
 
@@ -120,6 +120,36 @@ def test_linear_forms(ssdi8, M, O, K, dtype):
 
 
 # ------------------------------------------------------------------------------ selective scan
+FORMS = [  # B, L, heads, headdim, groups, N, tied, dtype, dt fp32, z, init, lengths
+    (2, 70, 66, 1, 2, 24, False, F16, False, True, True, [70, 3]),
+    (1, 300, 40, 1, 1, 32, False, BF16, True, True, True, None),        # cut into spans
+    (1, 40, 24, 1, 1, 20, False, F32, True, False, True, None),
+    (3, 129, 35, 1, 1, 32, False, F16, True, True, False, [0, 129, 64]),
+    (2, 65, 3, 64, 1, 64, True, F16, True, True, True, [64, 65]),
+    (1, 400, 4, 16, 2, 40, True, BF16, False, True, False, [390]),      # cut into spans
+    (2, 33, 2, 8, 1, 36, True, F32, True, False, True, None),
+    (1, 70, 5, 8, 1, 64, True, F16, False, False, False, None),
+    (2, 90, 40, 1, 1, 12, False, BF16, False, True, True, [90, 11]),
+]
+
+
+@pytest.mark.parametrize("B,L,H,P,G,N,tied,dtype,dt32,z,init,lengths", FORMS)
+def test_scan_forms(ssdi8, B, L, H, P, G, N, tied, dtype, dt32, z, init, lengths):
+    i = scan_inputs(Draw(L + H + N), B, L, H, P, G, N, tied, dtype, dt32, z, init)
+    n = torch.tensor(lengths, dtype=torch.int32) if lengths else None
+    y, e, h, he = scan_ref(i, lengths=n)
+    t = {k: None if v is None else v.clone() for k, v in i.items()}
+    if n is not None:
+        for k in ("u", "dt", "B", "C", "z"):
+            if t[k] is not None:
+                t[k][torch.arange(L)[None] >= n[:, None]] = float("nan")
+    g = {k: dev(v) for k, v in t.items()}
+    out = ssdi8.selective_scan(g["u"], g["dt"], g["A"], g["B"], g["C"], D=g["D"], z=g["z"],
+                               dt_bias=g["dt_bias"], init_state=g["state"], lengths=dev(n))
+    R.assert_within(out["y"], y, R.rounded(dtype, y, e), "y")
+    R.assert_within(out["final_state"], h, he + R.TINY[F32], "final_state")
+
+
 @pytest.mark.parametrize("L,H,P,G,N,tied,dtype", [
     (40, 24, 1, 1, 16, False, F16), (40, 24, 1, 1, 8, False, F16), (70, 24, 1, 1, 12, False, BF16),
     (300, 40, 1, 1, 24, False, F32),                                    # cut into spans
