@@ -200,3 +200,47 @@ def test_scan_infinite_state_over_spans(ssdi8, H, P, G, N, tied, dtype):
     out = ssdi8.selective_scan(g["u"], g["dt"], g["A"], g["B"], g["C"], D=g["D"], init_state=g["state"])
     R.assert_within(out["y"], y, R.rounded(dtype, y, e), "y")
     R.assert_within(out["final_state"], h, he + R.TINY[F32], "final_state")
+
+
+# ------------------------------------------------------------------------------ the followed calls
+SMALL = [{"op": "conv", "B": 2, "L": 70, "D": 21, "d1": 9, "d2": 8, "ragged": True, "state": True, "pad": 3},
+         {"op": "conv", "B": 3, "D": 40, "W": 3, "state": True, "step": True, "dtype": "bf16"},
+         {"op": "scan", "B": 2, "L": 40, "H": 16, "gate": True, "state": True, "ragged": True},
+         {"op": "scan", "B": 2, "L": 33, "H": 2, "P": 64, "N": 128, "tied": True, "dtype": "bf16"},
+         {"op": "scan", "B": 3, "H": 4, "P": 32, "G": 2, "N": 100, "tied": True, "state": True, "step": True},
+         {"op": "norm", "M": 5, "D": 96, "groups": 2, "gate": True, "residual": True, "pad": 7},
+         {"op": "norm", "M": 3, "D": 77, "gate": True, "before": True, "dtype": "fp32"},
+         {"op": "linear", "M": 9, "O": 33, "K": 200, "act": "gelu", "bias": True, "residual": True},
+         {"op": "linear", "M": 70, "O": 40, "K": 130, "dtype": "int8", "act": "softplus", "bias": True}]
+
+
+@pytest.mark.parametrize("case", SMALL, ids=lambda c: "-".join(str(v) for v in c.values()))
+def test_the_calls_64_bit_forms(ssdi8, case):
+    """The 64-bit results beside the calls whose speed is followed are those of block_ref.py: both are
+    64-bit sums of at most a few hundred terms, 2^-40 relative of the largest is far above either's
+    rounding and far below any other formula's."""
+    import perf.operators as P
+    got = P.exact(case, 5)
+    s = P.prepare(case, 5)
+    c = s["c"]
+    f = {k: v.double().cpu() if isinstance(v, torch.Tensor) and k != "lengths" else
+         v.cpu() if isinstance(v, torch.Tensor) else v for k, v in s.items()}
+    one = lambda k: f[k] if f[k] is None or not c["step"] else f[k][:, None]
+    if c["op"] == "conv":
+        y, _, last = R.conv(one("x"), f["w"], f["bias"], "silu", f["state"], f["lengths"])
+        want = (y[:, 0] if c["step"] else y), last
+        got = (got[0] if s["split"] is None else torch.cat(got[0], -1)), got[1]
+    elif c["op"] == "scan":
+        y, _, h, _ = R.scan(one("u"), one("dt"), f["A"], one("B"), one("C"), f["D"], one("z"), f["dt_bias"], True,
+                            f["state"], f["lengths"])
+        want = (y[:, 0] if c["step"] else y), h
+    elif c["op"] == "norm":
+        y, _, total = R.norm(f["x"], f["w"], f["z"], f["residual"], 1e-5, c["groups"], c["before"])
+        want = y, (total if f["residual"] is not None else None)
+    else:
+        want = R.linear(f["x"], f["w"], f["bias"], c["act"], f["residual"], f.get("x_scale"), f.get("w_scale"))[:1]
+        got = (got,)
+    for a, b in zip(got, want, strict=True):
+        assert (a is None) == (b is None)
+        if a is not None:
+            assert (a.cpu() - b).abs().max() <= 2.0 ** -40 * b.abs().max()
