@@ -119,6 +119,22 @@ def test_linear_forms(ssdi8, M, O, K, dtype):
     assert torch.equal(got.double(), want)
 
 
+@pytest.mark.parametrize("M", [3, 80])
+def test_gelu_of_negative_values(ssdi8, M):
+    """v (1 + erf(v / sqrt(2))) / 2 has relative accuracy for negative v too, where 1 + erf cancels.  The
+    exponential of -v^2 / 2 costs three roundings of its argument, 1.5 v^2 u in the result; the rest (a
+    reciprocal and a polynomial in it, whose slopes in the logarithm stay below 2.5, and the products) 28 u."""
+    v = torch.cat([torch.linspace(-12.0, 12.0, 4001), torch.tensor([0.0, -1e-20, 1e-6, -14.0, -40.0, -1e30, 1e30])])
+    y = 0.5 * v.double() * torch.erfc(-v.double() / 2 ** 0.5)
+    e = (1.5 * v.double().clamp(-20, 20) ** 2 + 28) * R.U * y.abs() + 16 * R.TINY[F32]
+    zero = lambda *s: torch.zeros(*s, dtype=F16, device="cuda")
+    got = ssdi8.linear(zero(M, 16), zero(v.numel(), 16), bias=dev(v), activation="gelu", y_dtype=F32)
+    R.assert_within(got, y.expand(M, -1), e.expand(M, -1), "y")
+    ends = ssdi8.linear(zero(M, 16), zero(2, 16), bias=torch.tensor([float("inf"), float("nan")], device="cuda"),
+                        activation="gelu", y_dtype=F32).cpu()
+    assert (ends[:, 0] == float("inf")).all() and torch.isnan(ends[:, 1]).all()
+
+
 # ------------------------------------------------------------------------------ selective scan
 FORMS = [  # B, L, heads, headdim, groups, N, tied, dtype, dt fp32, z, init, lengths
     (2, 70, 66, 1, 2, 24, False, F16, False, True, True, [70, 3]),
