@@ -460,8 +460,9 @@ hipError_t run_tile(const LinearArgs& a, hipStream_t st) {
 template <typename K> hipError_t run(const LinearArgs& a, hipStream_t st) {
   // Few rows.  Up to 16, one matrix tile of x: 8 x 10496 x 2560 bf16 13.1 us with 16 rows of w per workgroup,
   // 15.2 with 32 (8 x 2560 x 5120 9.2 / 14.6).  Up to 32, twice the rows of w where they still fill the card:
-  // 24 x 5120 x 2560 int8 8.0 / 6.9.  Up to 64, until the tiles below do: 64 x 2560 x 5120 24.9 (tiles 29.2),
-  // 40 x 10496 x 2560 28.6 (tiles 16.9).
+  // 24 x 5120 x 2560 int8 8.0 / 6.9.  Up to 64, while one round of workgroups does and the rows of x, which every
+  // workgroup reads, are short (33 x 2560 x 2560 fp16 10.6 us, tiles 10.9; 64 x 768 x 640 5.2, 5.6; 64 x 2560 x 5120
+  // 25.9, 20.2), or two rounds over a short k (48 x 6400 x 320 int8 4.6, 6.2; 33 x 8000 x 2560 fp16 19.2, 12.4).
   auto rows = [&](auto most, auto tiles) {
     constexpr int kMT = decltype(most)::value, kNT = decltype(tiles)::value;
     linear_rows<K, kNT, kMT, 8><<<dim3((unsigned)((a.n + 16 * kNT - 1) / (16 * kNT))), 512, 0, st>>>(a);
@@ -471,7 +472,9 @@ template <typename K> hipError_t run(const LinearArgs& a, hipStream_t st) {
   using Two = std::integral_constant<int, 2>;
   if (a.m <= 16) return rows(One(), One());
   if (a.m <= 32) return a.n >= 4096 ? rows(Two(), Two()) : rows(Two(), One());
-  if (a.m <= 64 && a.n < 64 * 128) return rows(std::integral_constant<int, 4>(), One());
+  const int64_t kbytes = a.k * (int64_t)sizeof(typename K::T);
+  if (a.m <= 64 && (a.n <= 256 * 16 ? a.m * kbytes <= 200000 : a.n < 2 * 256 * 16 && kbytes < 10 * kLine))
+    return rows(std::integral_constant<int, 4>(), One());
   // The tile whose rounds over the card's 256 CUs cost least: rounds * area / rate, the rates (of the
   // largest tile's) as 8192^3 in bf16 measured them: 898 us with 256 x 256, 986 with 256 x 192, 1030 with
   // 256 x 128, 1108 with 128 x 128, 1700 with 64 x 64.  Where another than the largest wins: 16384 x 768 x
@@ -496,7 +499,7 @@ template <typename K> hipError_t run(const LinearArgs& a, hipStream_t st) {
   // Small tiles that leave CUs without a second one, over a long k: four sets of waves share it (128 x 5120 x
   // 2560 fp16 16.3 -> 12.3 us, 200 x 2000 x 2000 12.1 -> 10.5, 100 x 768 x 1536 8.8 -> 7.8; over a short one their
   // ends cost more: 300 x 1111 x 1600 int8 8.7 -> 13.2).
-  const bool split = count(64, 64) <= 256 && a.k * (int64_t)sizeof(typename K::T) >= 24 * kLine;
+  const bool split = count(64, 64) <= 256 && kbytes >= 24 * kLine;
   return split ? run_tile<K, 64, 64, 2, 2, 4>(a, st) : run_tile<K, 64, 64, 2, 2>(a, st);
 }
 

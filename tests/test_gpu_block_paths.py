@@ -101,7 +101,7 @@ def test_norm_walks(ssdi8, M, D, groups, dtype, z, res, before):
 
 # ------------------------------------------------------------------------------ projections
 FEW = [(8, 70, 2600), (16, 4100, 2100), (24, 4100, 300), (32, 4111, 2600), (30, 70, 2600), (50, 100, 2600),
-       (64, 8190, 320), (40, 8200, 330)]
+       (64, 8190, 320), (40, 8200, 330), (64, 8190, 2600), (33, 4111, 1700), (63, 300, 6800), (48, 4096, 640)]
 SPLIT = [(65, 70, 3211), (1000, 1000, 3211), (130, 700, 6500)]
 
 
