@@ -465,7 +465,8 @@ ssdi8_status ssdi8_gated_norm(int64_t rows, int64_t channels, int64_t groups,
  *     y[r,o] = act(s sum_k x[r,k] weight[o,k] + bias[o]) + residual[r,o]
  * with s = 1 (fp16, bf16: products in fp32) or x_scale[r] weight_scale[o] (int8: products in int32; the
  * codes and per-token steps of ssdi8_quantize_act with SSDI8_GRAN_TOKEN, and weights quantized per
- * output).  y and the residual are fp32 or x's type (int8: fp16).  k >= 1, up to 131072 for int8.
+ * output).  y and the residual are fp32 or x's type (int8: fp16).  k >= 1, up to 131072 for int8, where one
+ * of x and weight holds no -128 (the quantizer gives none).
  * 256 rows of x, and of weight, span less than 4e9 bytes.
  */
 typedef struct {

@@ -45,7 +45,8 @@ class Projection:
 class Mamba2Block:
     """The SSD layer's block: x | B | C from one convolution, one decay per head, a gated norm behind
     the scan.  Whole chunks of a prompt run through the FP16 SSD layer, the rest through the selective
-    scan from the state that they leave; both keep the state in fp32.
+    scan from the state that they leave; both keep the state in fp32.  Activations are fp16, a batch's
+    prompts of one length; int8 is that of the projections.
 
     weights: norm (d), in_proj (2 di + 2 G N, d) for z, x, B, C, dt_proj (H, d), dt_bias (H),
     conv (di + 2 G N, W), conv_bias, A (H), D (H), gate_norm (di), out_proj (d, di); di = H * 64.

@@ -46,7 +46,8 @@ __device__ __forceinline__ void store_vec(T* p, int n, const float (&in)[kVec]) 
   }
 }
 
-// exp in the hardware's base 2 (one instruction, 1 ulp; results below the normal range are 0).
+// exp in the hardware's base 2: one instruction of 1 ulp; log2(e) and the product with it are rounded, so that
+// the result is within (2 |v| + 2) 2^-24 of its size.  Results below the normal range are 0.
 constexpr float kLog2eF = 1.44269504088896341f;
 __device__ __forceinline__ float fast_exp(float v) {
   return __builtin_amdgcn_exp2f(v * kLog2eF);

@@ -212,7 +212,7 @@ ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_
   if (a->y_dtype != SSDI8_F32 && a->y_dtype != own) return SSDI8_ERR_ARG;
   if (a->act < SSDI8_ACT_NONE || a->act > SSDI8_ACT_SOFTPLUS) return SSDI8_ERR_ARG;
   if (!quantized && (a->x_scale || a->weight_scale)) return SSDI8_ERR_ARG;
-  if (quantized && k > 131072) return SSDI8_ERR_UNSUPPORTED;   // 127^2 k stays below 2^31
+  if (quantized && k > 131072) return SSDI8_ERR_UNSUPPORTED;   // 127 * 128 k stays below 2^31
   if (bad_stride(a->x_row_stride) || bad_stride(a->weight_row_stride) ||
       bad_stride(a->residual_row_stride) || a->y_row_stride < outputs || bad_stride(a->y_row_stride))
     return SSDI8_ERR_SHAPE;

@@ -7,7 +7,7 @@
 // channels, its weights and the last W-1 rows in registers and walks kTokens tokens, so a row is read
 // once except for the W-1 rows in front of each walk (from the L2 cache).  64 lanes lie along the
 // channels: 1 KB of a row per access.  4 x 4096 x 5376 fp16, columns of rows twice as wide into three
-// outputs: 78 us, 4.5 TB/s (a copy of the same rows 64).  A token of 8
+// outputs: 83 us, 4.3 TB/s (78 on inputs that stay the same; a copy of the same rows 64).  A token of 8
 // sequences: 4 us, a launch and one chain of loads.
 #include <type_traits>
 

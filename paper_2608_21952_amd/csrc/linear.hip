@@ -11,12 +11,12 @@
 // in whole lines.
 // What bounds it: the matrix unit and the way of the operands into it, which do not overlap in full: taken
 // apart (8192^3 bf16, loads straight to LDS at that time, 1070 us in all) the products with their fragment
-// reads took 703 us, the loads with the reads 802.  int8 16384 x 10496 x 2560 475 us (1.85 Pop/s; the vendor's
-// library 472 without the epilogue), fp16 16384 x 768 x 1536 with residual 46 us (0.85 PFLOP/s; 42), fp16
-// 16384 x 10496 x 2560 830 us (779).
+// reads took 703 us, the loads with the reads 802.  int8 16384 x 10496 x 2560 472 us (1.87 Pop/s; the vendor's
+// library 472 without the epilogue), fp16 16384 x 768 x 1536 with residual 52 us (0.74 PFLOP/s; 42 without it; 61
+// where neither inputs nor outputs are in the cache), fp16 16384 x 10496 x 2560 830 us (779).
 // Few rows (linear_rows): bound by the bytes of w.  A workgroup takes 16 or 32 rows of w, its waves share k
 // by lines of 128 bytes, each straight from memory into the matrix instruction's registers, and their sums
-// meet in LDS.  8 x 10496 x 2560 bf16: 13.1 us, 4.1 TB/s, near the time that the first loads take to arrive.
+// meet in LDS.  8 x 10496 x 2560 bf16: 13.0 us, 4.1 TB/s, near the time that the first loads take to arrive.
 // What lies behind a row's end in its last k-tile or line becomes 0 in both operands; rows may start at any
 // element.
 #include <type_traits>

@@ -16,8 +16,8 @@
 // What bounds it: the vector unit.  Per (token, channel, state) one exponential at half rate and four
 // full-rate operations (three alone where the decay is tied), 61 us over the card's 1024 SIMDs for 8 x 2048 x
 // 1536 x 16; softplus, gate and conversions of every element take about as long as half of that, the sums
-// over a channel's lanes a quarter.  Measured there 196 us (fp16 with gate; 1.5 workgroups per CU, so that the
-// fuller ones decide), 503 us for 4 x 4096 x 5120 x 16 in bf16, 220 us for one fp32 prompt of 16384 x 1536, 36 us
+// over a channel's lanes a quarter.  Measured there 197 us (fp16 with gate; 1.5 workgroups per CU, so that the
+// fuller ones decide), 504 us for 4 x 4096 x 5120 x 16 in bf16, 220 us for one fp32 prompt of 16384 x 1536, 36 us
 // for three remainders of 201 tokens, 24 heads of 64 x 128.
 //
 // Everything is held in fp32; y is rounded once.  Tokens at or behind a sequence's length count as
