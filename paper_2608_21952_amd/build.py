@@ -28,7 +28,8 @@ SOURCES = ["api.hip", "quantize.hip", "chunk_bmm.hip", "chunk_state.hip", "state
            "chunk_scan.hip", "decode.hip", "fp16_bmm.hip", "fp16_state.hip",
            "fp16_scan.hip", "fp16_walk.hip", "calibrate.hip", "probe.hip", "conv.hip",
            "selective_scan.hip", "selective_scan_fast.hip", "norm.hip", "linear.hip",
-           "block_api.hip"]
+           "block_api.hip", "linear_attention.hip", "norm_quantize.hip", "quantize_mx.hip",
+           "linear_mx.hip", "mixer_api.hip"]
 
 # -ffp-contract=off: no fused multiply-add where the arithmetic defines separate roundings.
 # -packed-fp32-ops off: never emit packed fp32 arithmetic.

@@ -10,6 +10,9 @@
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
+
 #include "ssdi8.h"
 
 namespace {
@@ -25,6 +28,12 @@ decltype(&ssdi8_selective_scan) g_sel_scan = nullptr;
 decltype(&ssdi8_selective_scan_step) g_sel_scan_step = nullptr;
 decltype(&ssdi8_gated_norm) g_norm = nullptr;
 decltype(&ssdi8_linear) g_linear = nullptr;
+decltype(&ssdi8_linear_attention_workspace_size) g_attention_size = nullptr;
+decltype(&ssdi8_linear_attention) g_attention = nullptr;
+decltype(&ssdi8_linear_attention_step) g_attention_step = nullptr;
+decltype(&ssdi8_norm_quantize) g_norm_quantize = nullptr;
+decltype(&ssdi8_quantize_mx) g_quantize_mx = nullptr;
+decltype(&ssdi8_linear_mx) g_linear_mx = nullptr;
 c10::DeviceType g_device = c10::DeviceType::CUDA;   // where its tensors live
 
 // Thrown (and caught at the entry) for arguments that belong to the Python path.
@@ -638,6 +647,253 @@ PyObject* linear(PyObject*, PyObject* const* o, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------------------------- mixer and few bits
+// bind_mixer(linear_attention_workspace_size, linear_attention, linear_attention_step, norm_quantize, quantize_mx,
+// linear_mx): the library's addresses, after bind
+PyObject* bind_mixer(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 6) {
+    PyErr_SetString(PyExc_TypeError, "bind_mixer takes 6 addresses");
+    return nullptr;
+  }
+  void* p[6];
+  for (int i = 0; i < 6; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (!p[i]) {
+      if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
+      return nullptr;
+    }
+  }
+  g_attention_size = reinterpret_cast<decltype(g_attention_size)>(p[0]);
+  g_attention = reinterpret_cast<decltype(g_attention)>(p[1]);
+  g_attention_step = reinterpret_cast<decltype(g_attention_step)>(p[2]);
+  g_norm_quantize = reinterpret_cast<decltype(g_norm_quantize)>(p[3]);
+  g_quantize_mx = reinterpret_cast<decltype(g_quantize_mx)>(p[4]);
+  g_linear_mx = reinterpret_cast<decltype(g_linear_mx)>(p[5]);
+  Py_RETURN_NONE;
+}
+
+// All on the device of the first: the Python path names the one that is not.
+void same_device(const at::Tensor& t, std::initializer_list<PyObject*> others) {
+  for (PyObject* o : others)
+    if (o != Py_None && (!THPVariable_CheckExact(o) || THPVariable_Unpack(o).device() != t.device()))
+      throw NotPlain();
+}
+
+// The arguments that both forms of linear attention share: q, k, v, log_decay, scale.
+void attention_args(ssdi8_attn_dims& d, ssdi8_attn_args& a, const at::Tensor& q, PyObject* const* o) {
+  const bool step = q.dim() == 3;
+  const at::Tensor& k = rows(o[1]);
+  const at::Tensor& v = rows(o[2]);
+  if (k.dim() != q.dim() || v.dim() != q.dim()) throw NotPlain();
+  const int64_t b = q.size(0), L = step ? 1 : q.size(1);
+  d = {b, L, q.size(-2), k.size(-2), v.size(-2), q.size(-1), v.size(-1)};
+  auto same = [&](const at::Tensor& t) {
+    if (t.scalar_type() != q.scalar_type() || t.size(0) != b || (!step && t.size(1) != L)) throw NotPlain();
+  };
+  same(k);
+  same(v);
+  if (k.size(-1) != d.keys) throw NotPlain();
+  a.dtype = activation_code(q);
+  auto token = [&](const at::Tensor& t) { return step ? (int64_t)0 : t.stride(1); };
+  a.q = q.data_ptr(), a.q_batch_stride = q.stride(0), a.q_token_stride = token(q), a.q_head_stride = q.stride(-2);
+  a.k = k.data_ptr(), a.k_batch_stride = k.stride(0), a.k_token_stride = token(k), a.k_head_stride = k.stride(-2);
+  a.v = v.data_ptr(), a.v_batch_stride = v.stride(0), a.v_token_stride = token(v), a.v_head_stride = v.stride(-2);
+  if (o[3] != Py_None) {
+    const at::Tensor& g = rows(o[3]);
+    if (g.scalar_type() != at::kFloat) throw NotPlain();
+    a.token_decay = g.dim() != 1;
+    if (a.token_decay) {
+      if (!(step ? has_shape(g, {b, d.v_heads}) : has_shape(g, {b, L, d.v_heads}))) throw NotPlain();
+      a.decay_batch_stride = g.stride(0);
+      a.decay_token_stride = token(g);
+    } else if (g.size(0) != d.v_heads) {
+      throw NotPlain();
+    }
+    a.log_decay = static_cast<float*>(g.data_ptr());
+  }
+  if (o[4] == Py_None) a.scale = (float)(1.0 / std::sqrt((double)d.keys));
+  else if (PyFloat_Check(o[4])) a.scale = (float)PyFloat_AS_DOUBLE(o[4]);
+  else throw NotPlain();
+}
+
+// attention(q, k, v, log_decay, scale, init, lengths, final_state, stream) -> (status, y, final_state or None)
+PyObject* attention(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 9 || !g_attention) throw NotPlain();
+    const at::Tensor& q = rows(o[0]);
+    if (q.dim() != 4) throw NotPlain();
+    same_device(q, {o[1], o[2], o[3], o[5], o[6]});
+    ssdi8_attn_dims d;
+    ssdi8_attn_args a = {};
+    attention_args(d, a, q, o);
+    a.init_state = floats_or_null(o[5], {d.batch, d.v_heads, d.keys, d.values});
+    a.lengths = ints_or_null(o[6], {d.batch});
+    void* st = stream_of(o[8]);
+    at::Tensor y = empty(q, q.scalar_type(), {d.batch, d.seqlen, std::max(d.q_heads, d.v_heads), d.values}), last, ws;
+    a.y = y.data_ptr();
+    if (integer(o[7])) {
+      last = empty(q, at::kFloat, {d.batch, d.v_heads, d.keys, d.values});
+      a.final_state = static_cast<float*>(last.data_ptr());
+    }
+    const size_t need = g_attention_size(&d, a.dtype);
+    if (need) {
+      ws = empty(q, at::kByte, {(int64_t)need});
+      a.workspace = ws.data_ptr();
+      a.workspace_bytes = need;
+    }
+    const ssdi8_status s = released([&] { return g_attention(&d, &a, st); });
+    return Py_BuildValue("(iNN)", (int)s, THPVariable_Wrap(y), wrap_or_none(last));
+  });
+}
+
+// attention_step(q, k, v, log_decay, scale, state, stream) -> (status, y)
+PyObject* attention_step(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 7 || !g_attention_step) throw NotPlain();
+    const at::Tensor& q = rows(o[0]);
+    if (q.dim() != 3) throw NotPlain();
+    same_device(q, {o[1], o[2], o[3], o[5]});
+    ssdi8_attn_dims d;
+    ssdi8_attn_args a = {};
+    attention_args(d, a, q, o);
+    a.final_state = floats(o[5], {d.batch, d.v_heads, d.keys, d.values});
+    void* st = stream_of(o[6]);
+    at::Tensor y = empty(q, q.scalar_type(), {d.batch, std::max(d.q_heads, d.v_heads), d.values});
+    a.y = y.data_ptr();
+    const ssdi8_status s = released([&] { return g_attention_step(&d, &a, st); });
+    return Py_BuildValue("(iN)", (int)s, THPVariable_Wrap(y));
+  });
+}
+
+// Codes and scales for the rows of t, k values each.
+void empty_codes(const at::Tensor& t, int64_t k, int format, at::Tensor& codes, at::Tensor& scales) {
+  if (format == SSDI8_FMT_I8) {
+    codes = empty_like_rows(t, at::kChar, k);
+    c10::SmallVector<int64_t, 5> s(t.sizes().begin(), t.sizes().end() - 1);
+    NoGil no_gil;
+    scales = at::empty(s, t.options().dtype(at::kFloat).requires_grad(false));
+    return;
+  }
+  if (format != SSDI8_FMT_MXFP8 && format != SSDI8_FMT_MXFP4) throw NotPlain();
+  const int64_t blocks = (k + 31) / 32;
+  codes = format == SSDI8_FMT_MXFP8 ? empty_like_rows(t, at::kFloat8_e4m3fn, blocks * 32)
+                                    : empty_like_rows(t, at::kByte, blocks * 16);
+  scales = empty_like_rows(t, at::kFloat8_e8m0fnu, blocks);
+}
+
+// norm_quantize(x, weight, z, residual, eps, groups, norm_before_gate, format, with_y, residual_out, stream)
+//   -> (status, codes, scales, y or None, residual_out or None)
+PyObject* norm_quantize(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 11 || !g_norm_quantize) throw NotPlain();
+    const at::Tensor& x = rows(o[0]);
+    same_device(x, {o[1], o[2], o[3], o[9]});
+    const Flat f(x);
+    const int64_t D = x.size(-1);
+    ssdi8_norm_quant_args a = {};
+    a.dtype = activation_code(x);
+    a.x = x.data_ptr();
+    a.x_row_stride = f.stride;
+    a.weight = floats(o[1], {D});
+    if (o[2] != Py_None) {
+      const at::Tensor& z = rows(o[2]);
+      if (z.scalar_type() != x.scalar_type() || !z.sizes().equals(x.sizes())) throw NotPlain();
+      a.z = z.data_ptr();
+      a.z_row_stride = Flat(z).stride;
+    }
+    if (!PyFloat_Check(o[4])) throw NotPlain();
+    a.eps = (float)PyFloat_AS_DOUBLE(o[4]);
+    const int64_t groups = integer(o[5]);
+    a.norm_before_gate = (int)integer(o[6]);
+    a.format = (int)integer(o[7]);
+    auto dense = [&](PyObject* t) -> const at::Tensor& {
+      const at::Tensor& v = tensor(t, x.scalar_type());
+      if (!v.sizes().equals(x.sizes())) throw NotPlain();
+      return v;
+    };
+    void* st = stream_of(o[10]);
+    at::Tensor sum, y, codes, scales;
+    if (o[3] != Py_None) {
+      a.residual = dense(o[3]).data_ptr();
+      sum = o[9] == Py_None ? empty_like_rows(x, x.scalar_type(), D) : dense(o[9]);
+      a.residual_out = sum.data_ptr();
+    } else if (o[9] != Py_None) {
+      throw NotPlain();
+    }
+    if (integer(o[8])) {
+      y = empty_like_rows(x, x.scalar_type(), D);
+      a.y = y.data_ptr();
+    }
+    empty_codes(x, D, a.format, codes, scales);
+    a.codes = codes.data_ptr();
+    a.scales = scales.data_ptr();
+    const ssdi8_status s = released([&] { return g_norm_quantize(f.count, D, groups, &a, st); });
+    return Py_BuildValue("(iNNNN)", (int)s, THPVariable_Wrap(codes), THPVariable_Wrap(scales), wrap_or_none(y),
+                         wrap_or_none(sum));
+  });
+}
+
+// quantize_mx(x, format, stream) -> (status, codes, scales)
+PyObject* quantize_mx(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 3 || !g_quantize_mx) throw NotPlain();
+    const at::Tensor& x = rows(o[0]);
+    const Flat f(x);
+    const int64_t K = x.size(-1);
+    const int dtype = activation_code(x), format = (int)integer(o[1]);
+    if (format == SSDI8_FMT_I8) throw NotPlain();
+    void* st = stream_of(o[2]);
+    at::Tensor codes, scales;
+    empty_codes(x, K, format, codes, scales);
+    const void* from = x.data_ptr();
+    void *to = codes.data_ptr(), *steps = scales.data_ptr();
+    const ssdi8_status s =
+        released([&] { return g_quantize_mx(f.count, K, from, dtype, f.stride, format, to, steps, st); });
+    return Py_BuildValue("(iNN)", (int)s, THPVariable_Wrap(codes), THPVariable_Wrap(scales));
+  });
+}
+
+// linear_mx(x codes, x scales, weight codes, weight scales, bias, act, residual, y_dtype, stream) -> (status, y)
+PyObject* linear_mx(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    if (n != 9 || !g_linear_mx) throw NotPlain();
+    const at::Tensor& x = any_tensor(o[0]);
+    same_device(x, {o[1], o[2], o[3], o[4], o[6]});
+    const at::Tensor& xs = tensor(o[1], at::kFloat8_e8m0fnu);
+    const at::Tensor& w = tensor(o[2], at::kByte);
+    if (x.dim() < 2 || x.numel() == 0 || w.dim() != 2 || w.numel() == 0) throw NotPlain();
+    const bool four = x.scalar_type() == at::kByte;
+    if (!four && x.scalar_type() != at::kFloat8_e4m3fn) throw NotPlain();
+    const int64_t k = x.size(-1) * (four ? 2 : 1), O = w.size(0);
+    if (k % 32 != 0 || w.size(1) * 2 != k || xs.size(-1) != k / 32 || !same_lead(xs, x)) throw NotPlain();
+    ssdi8_linear_mx_args a = {};
+    a.x_format = four ? SSDI8_FMT_MXFP4 : SSDI8_FMT_MXFP8;
+    a.x_codes = x.data_ptr();
+    a.x_scales = xs.data_ptr();
+    a.weight_codes = w.data_ptr();
+    a.weight_scales = shaped(o[3], at::kFloat8_e8m0fnu, {O, k / 32});
+    a.bias = floats_or_null(o[4], {O});
+    a.act = (int)integer(o[5]);
+    a.y_dtype = (int)integer(o[7]);
+    const at::ScalarType ydt = a.y_dtype == SSDI8_F32 ? at::kFloat
+                               : a.y_dtype == SSDI8_F16 ? at::kHalf
+                               : a.y_dtype == SSDI8_BF16 ? at::kBFloat16 : throw NotPlain();
+    if (o[6] != Py_None) {
+      const at::Tensor& r = rows(o[6]);
+      if (r.scalar_type() != ydt || r.size(-1) != O || !same_lead(r, x)) throw NotPlain();
+      a.residual = r.data_ptr();
+      a.residual_row_stride = Flat(r).stride;
+    }
+    void* st = stream_of(o[8]);
+    const int64_t M = x.numel() / x.size(-1);
+    at::Tensor y = empty_like_rows(x, ydt, O);
+    a.y = y.data_ptr();
+    a.y_row_stride = O;
+    const ssdi8_status s = released([&] { return g_linear_mx(M, O, k, &a, st); });
+    return Py_BuildValue("(iN)", (int)s, THPVariable_Wrap(y));
+  });
+}
+
 #define SSDI8_FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL
 PyMethodDef methods[] = {
     {"bind", SSDI8_FAST(bind), "bind(quantize_act, ssd_workspace_size, ssd_chunk_scan, decode_step, device)"},
@@ -653,6 +909,14 @@ PyMethodDef methods[] = {
     {"sel_scan_step", SSDI8_FAST(sel_scan_step), "ssdi8_selective_scan_step"},
     {"norm", SSDI8_FAST(norm), "ssdi8_gated_norm"},
     {"linear", SSDI8_FAST(linear), "ssdi8_linear"},
+    {"bind_mixer", SSDI8_FAST(bind_mixer),
+     "bind_mixer(linear_attention_workspace_size, linear_attention, linear_attention_step, norm_quantize, "
+     "quantize_mx, linear_mx)"},
+    {"attention", SSDI8_FAST(attention), "ssdi8_linear_attention"},
+    {"attention_step", SSDI8_FAST(attention_step), "ssdi8_linear_attention_step"},
+    {"norm_quantize", SSDI8_FAST(norm_quantize), "ssdi8_norm_quantize"},
+    {"quantize_mx", SSDI8_FAST(quantize_mx), "ssdi8_quantize_mx"},
+    {"linear_mx", SSDI8_FAST(linear_mx), "ssdi8_linear_mx"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -14,7 +14,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import os
-from typing import Dict, Iterable, Optional, Tuple
+from typing import Dict, Iterable, NamedTuple, Optional, Tuple, Union
 
 import torch
 
@@ -134,6 +134,45 @@ class LinearArgs(ctypes.Structure):
     ]
 
 
+class AttnDims(ctypes.Structure):
+    _fields_ = [(n, _L) for n in
+                ("batch", "seqlen", "q_heads", "k_heads", "v_heads", "keys", "values")]
+
+
+class AttnArgs(ctypes.Structure):
+    _fields_ = [("dtype", _I)] + [
+        f for t in ("q", "k", "v")
+        for f in ((t, _P), (t + "_batch_stride", _L), (t + "_token_stride", _L), (t + "_head_stride", _L))] + [
+        ("log_decay", _P), ("token_decay", _I), ("decay_batch_stride", _L), ("decay_token_stride", _L),
+        ("scale", ctypes.c_float), ("init_state", _P), ("lengths", _P), ("y", _P), ("final_state", _P),
+        ("workspace", _P), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class NormQuantArgs(ctypes.Structure):
+    _fields_ = [
+        ("dtype", _I), ("x", _P), ("x_row_stride", _L), ("z", _P), ("z_row_stride", _L),
+        ("residual", _P), ("weight", _P), ("eps", ctypes.c_float), ("norm_before_gate", _I),
+        ("format", _I), ("codes", _P), ("scales", _P), ("y", _P), ("residual_out", _P),
+    ]
+
+
+class LinearMxArgs(ctypes.Structure):
+    _fields_ = [
+        ("x_format", _I), ("x_codes", _P), ("x_scales", _P), ("weight_codes", _P), ("weight_scales", _P),
+        ("bias", _P), ("act", _I), ("residual", _P), ("residual_row_stride", _L), ("y", _P),
+        ("y_row_stride", _L), ("y_dtype", _I),
+    ]
+
+
+class Mx(NamedTuple):
+    """Rows of values in blocks of 32 that share a power of two (quantize_mx, norm_quantize, linear_mx): codes
+    float8_e4m3fn (..., K) ("mxfp8") or uint8 (..., K / 2) with two e2m1 codes to a byte, the even one in the low half
+    ("mxfp4"); scales float8_e8m0fnu (..., K / 32).  K is filled up with zeros to whole blocks."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+
+
 _lib = None
 _native = None    # the native marshalling, loaded with the library
 
@@ -190,6 +229,19 @@ def lib() -> ctypes.CDLL:
     L.ssdi8_gated_norm.restype = _I
     L.ssdi8_linear.argtypes = [i64, i64, i64, ctypes.POINTER(LinearArgs), _P]
     L.ssdi8_linear.restype = _I
+    attn = [ctypes.POINTER(AttnDims), ctypes.POINTER(AttnArgs), _P]
+    L.ssdi8_linear_attention_workspace_size.argtypes = [ctypes.POINTER(AttnDims), _I]
+    L.ssdi8_linear_attention_workspace_size.restype = ctypes.c_size_t
+    L.ssdi8_linear_attention.argtypes = attn
+    L.ssdi8_linear_attention.restype = _I
+    L.ssdi8_linear_attention_step.argtypes = attn
+    L.ssdi8_linear_attention_step.restype = _I
+    L.ssdi8_norm_quantize.argtypes = [i64, i64, i64, ctypes.POINTER(NormQuantArgs), _P]
+    L.ssdi8_norm_quantize.restype = _I
+    L.ssdi8_quantize_mx.argtypes = [i64, i64, _P, _I, i64, _I, _P, _P, _P]
+    L.ssdi8_quantize_mx.restype = _I
+    L.ssdi8_linear_mx.argtypes = [i64, i64, i64, ctypes.POINTER(LinearMxArgs), _P]
+    L.ssdi8_linear_mx.restype = _I
     L.ssdi8_status_string.argtypes = [_I]
     L.ssdi8_status_string.restype = ctypes.c_char_p
     L.ssdi8_version.argtypes = []
@@ -202,6 +254,9 @@ def lib() -> ctypes.CDLL:
                         addr(L.ssdi8_selective_scan_workspace_size), addr(L.ssdi8_selective_scan),
                         addr(L.ssdi8_selective_scan_step), addr(L.ssdi8_gated_norm),
                         addr(L.ssdi8_linear))
+    _binding.bind_mixer(addr(L.ssdi8_linear_attention_workspace_size), addr(L.ssdi8_linear_attention),
+                        addr(L.ssdi8_linear_attention_step), addr(L.ssdi8_norm_quantize),
+                        addr(L.ssdi8_quantize_mx), addr(L.ssdi8_linear_mx))
     _native = _binding
     _lib = L
     return L
@@ -1042,6 +1097,302 @@ def linear(x: torch.Tensor, weight: torch.Tensor, *, bias: Optional[torch.Tensor
         rr = _rows(_flat(residual, "residual"), "residual", y_dtype, (M, O))
         a.residual, a.residual_row_stride = _ptr(rr), rr.stride(0)
     _check(lib().ssdi8_linear(M, O, K, ctypes.byref(a), _stream(stream)), "ssdi8_linear")
+    return y
+
+
+# ------------------------------------------------------------------------------ mixer and few bits
+FORMAT = {"int8": 0, "mxfp8": 1, "mxfp4": 2}
+_CODES = {"int8": torch.int8, "mxfp8": torch.float8_e4m3fn, "mxfp4": torch.uint8}
+MX_BLOCK = 32
+
+
+def _here(x) -> bool:
+    """Whether a native call may be tried: _plain, and x lies on the current device."""
+    return _plain(x) and x.get_device() == torch._C._cuda_getDevice()
+
+
+@contextlib.contextmanager
+def _device_of(x: torch.Tensor, stream, *others):
+    """Runs on the device of x, where all tensors have to be; a stream that is given belongs to it."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError("a device tensor is needed")
+    for t in others:
+        if isinstance(t, torch.Tensor) and t.device != x.device:
+            raise ValueError(f"all tensors must be on {x.device}, got one on {t.device}")
+    if isinstance(stream, torch.cuda.Stream) and stream.device != x.device:
+        raise ValueError(f"the stream must be one of {x.device}")
+    with torch.cuda.device(x.device):
+        yield
+
+
+def _attention(q, k, v, log_decay, scale, y, stream):
+    """The arguments that the two forms of linear attention share, their sizes, and y."""
+    _activation_type(q, "q", q.dim() if q.dim() in (3, 4) else 4)
+    lead = tuple(q.shape[:-2])
+    for t, name in ((k, "k"), (v, "v")):
+        if not isinstance(t, torch.Tensor) or t.dim() != q.dim():
+            raise ValueError(f"{name} must have {q.dim()} dimensions")
+    Hq, K = q.shape[-2:]
+    Hk, (Hv, V) = k.shape[-2], v.shape[-2:]
+    d = AttnDims(lead[0], lead[1] if len(lead) == 2 else 1, Hq, Hk, Hv, K, V)
+    a = AttnArgs()
+    a.dtype = _DTYPES[q.dtype]
+    for name, t, shape in (("q", q, (*lead, Hq, K)), ("k", k, (*lead, Hk, K)), ("v", v, (*lead, Hv, V))):
+        _rows(t, name, q.dtype, shape)
+        setattr(a, name, _ptr(t))
+        setattr(a, name + "_batch_stride", t.stride(0))
+        setattr(a, name + "_head_stride", t.stride(-2))
+        if len(lead) == 2:
+            setattr(a, name + "_token_stride", t.stride(1))
+    if log_decay is not None:
+        a.token_decay = int(log_decay.dim() != 1)
+        g = _rows(log_decay, "log_decay", torch.float32, (*lead, Hv) if a.token_decay else (Hv,))
+        a.log_decay = _ptr(g)
+        if a.token_decay:
+            a.decay_batch_stride = g.stride(0)
+            if len(lead) == 2:
+                a.decay_token_stride = g.stride(1)
+    a.scale = K ** -0.5 if scale is None else float(scale)
+    shape = (*lead, max(Hq, Hv), V)
+    if y is None:
+        with _on(stream):
+            y = torch.empty(shape, dtype=q.dtype, device=q.device)
+    a.y = _ptr(_need(y, "y", q.dtype, shape))
+    return d, a, y
+
+
+def linear_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                     log_decay: Optional[torch.Tensor] = None, *, scale: Optional[float] = None,
+                     init_state: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                     y: Optional[torch.Tensor] = None, final_state: bool = True,
+                     workspace: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """Linear attention with a decay per head at any length (ssdi8_linear_attention): per head
+    S = exp(log_decay) S + k v^T, y = scale S^T q.  q (b,L,Hq,K), k (b,L,Hk,K), v (b,L,Hv,V) fp16, bf16 or
+    fp32 at any strides of batch, token and head, K up to 256; log_decay fp32, at most 0, (Hv), or (b,L,Hv) per
+    token, or None; scale 1/sqrt(K) unless given; init_state (b,Hv,K,V) fp32, lengths (b) int32.  y has
+    max(Hq,Hv) heads, which Hq and Hv divide; Hk divides Hv; neighbouring heads share one.
+    Returns y (b,L,max(Hq,Hv),V) and, with final_state, the state after the last token (b,Hv,K,V) fp32."""
+    if y is None and workspace is None and stream is None and _here(q):
+        r = _native.attention(q, k, v, log_decay, scale, init_state, lengths, int(final_state),
+                              _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_linear_attention")
+            return {"y": r[1], "final_state": r[2]} if final_state else {"y": r[1]}
+    with _device_of(q, stream, k, v, log_decay, init_state, lengths, y, workspace):
+        _activation_type(q, "q", 4)
+        d, a, y = _attention(q, k, v, log_decay, scale, y, stream)
+        state = (d.batch, d.v_heads, d.keys, d.values)
+        a.init_state = _param(init_state, "init_state", state)
+        if lengths is not None:
+            a.lengths = _ptr(_need(lengths, "lengths", torch.int32, (d.batch,)))
+        out = {"y": y}
+        need = linear_attention_workspace_size(d, q.dtype)
+        with _on(stream):
+            if final_state:
+                out["final_state"] = torch.empty(state, dtype=torch.float32, device=q.device)
+                a.final_state = _ptr(out["final_state"])
+            if workspace is None and need:
+                workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        if workspace is not None:
+            _need(workspace, "workspace", torch.uint8)
+            a.workspace, a.workspace_bytes = _ptr(workspace), workspace.numel()
+        _check(lib().ssdi8_linear_attention(ctypes.byref(d), ctypes.byref(a), _stream(stream)),
+               "ssdi8_linear_attention")
+    return out
+
+
+def linear_attention_workspace_size(d: AttnDims, dtype: torch.dtype) -> int:
+    return int(lib().ssdi8_linear_attention_workspace_size(ctypes.byref(d), _DTYPES[dtype]))
+
+
+def linear_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, state: torch.Tensor,
+                          log_decay: Optional[torch.Tensor] = None, *, scale: Optional[float] = None,
+                          y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """One token of linear_attention (ssdi8_linear_attention_step): q (b,Hq,K), k (b,Hk,K), v (b,Hv,V), log_decay
+    (Hv), or (b,Hv), or None; state (b,Hv,K,V) fp32 is updated in place.  Returns y (b,max(Hq,Hv),V)."""
+    if y is None and stream is None and _here(q):
+        r = _native.attention_step(q, k, v, log_decay, scale, state, _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_linear_attention_step")
+            return r[1]
+    with _device_of(q, stream, k, v, log_decay, state, y):
+        _activation_type(q, "q", 3)
+        d, a, y = _attention(q, k, v, log_decay, scale, y, stream)
+        a.final_state = _param(state, "state", (d.batch, d.v_heads, d.keys, d.values))
+        _check(lib().ssdi8_linear_attention_step(ctypes.byref(d), ctypes.byref(a), _stream(stream)),
+               "ssdi8_linear_attention_step")
+    return y
+
+
+def _format(name, allowed) -> int:
+    if name not in allowed:
+        raise ValueError(f"format must be one of {', '.join(allowed)}, got {name!r}")
+    return FORMAT[name]
+
+
+def _code_shapes(lead, k: int, format: str):
+    """Shapes and types of the codes and the scales of rows of k values."""
+    if format == "int8":
+        return (*lead, k), lead, torch.float32
+    blocks = -(-k // MX_BLOCK)
+    return (*lead, blocks * MX_BLOCK // (2 if format == "mxfp4" else 1)), (*lead, blocks), torch.float8_e8m0fnu
+
+
+def norm_quantize(x: torch.Tensor, weight: torch.Tensor, *, z: Optional[torch.Tensor] = None,
+                  residual: Optional[torch.Tensor] = None, eps: float = 1e-5, groups: int = 1,
+                  norm_before_gate: bool = False, format: str = "int8", with_y: bool = False,
+                  residual_out: Optional[torch.Tensor] = None, stream=None) -> Dict[str, torch.Tensor]:
+    """gated_norm with its output in few bits (ssdi8_norm_quantize): x, z, residual (..., D), weight (D), D up to
+    32768.  format "int8": codes (..., D) and a step per row, scales (...) fp32: x and x_scale of linear.
+    "mxfp8", "mxfp4": codes and scales as those of Mx, for linear_mx.  Returns codes, scales, with with_y also y in
+    x's type, and, with a residual, the sum x + residual (in residual_out, which may be the residual itself, or a new
+    tensor)."""
+    fmt = _format(format, ("int8", "mxfp8", "mxfp4"))
+    if stream is None and _here(x):
+        r = _native.norm_quantize(x, weight, z, residual, eps, groups, int(norm_before_gate), fmt, int(with_y),
+                                  residual_out, _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_norm_quantize")
+            out = {"codes": r[1], "scales": r[2]}
+            if with_y:
+                out["y"] = r[3]
+            if residual is not None:
+                out["residual"] = r[4] if residual_out is None else residual_out
+            return out
+    with _device_of(x, stream, weight, z, residual, residual_out):
+        lead = tuple(x.shape[:-1])
+        xr = _flat(x, "x")
+        _activation_type(xr, "x", 2)
+        M, D = xr.shape
+        _rows(xr, "x", x.dtype, (M, D))
+        a = NormQuantArgs()
+        a.dtype, a.x, a.x_row_stride = _DTYPES[x.dtype], _ptr(xr), xr.stride(0)
+        if z is not None:
+            zr = _rows(_flat(z, "z"), "z", x.dtype, (M, D))
+            a.z, a.z_row_stride = _ptr(zr), zr.stride(0)
+        a.weight = _param(weight, "weight", (D,))
+        a.eps, a.norm_before_gate, a.format = float(eps), int(norm_before_gate), fmt
+        codes, scales, stype = _code_shapes(lead, D, format)
+        with _on(stream):
+            out = {"codes": torch.empty(codes, dtype=_CODES[format], device=x.device),
+                   "scales": torch.empty(scales, dtype=stype, device=x.device)}
+            if with_y:
+                out["y"] = torch.empty(*lead, D, dtype=x.dtype, device=x.device)
+            if residual is not None and residual_out is None:
+                residual_out = torch.empty(*lead, D, dtype=x.dtype, device=x.device)
+        a.codes, a.scales, a.y = _ptr(out["codes"]), _ptr(out["scales"]), _ptr(out.get("y"))
+        if residual is not None:
+            a.residual = _ptr(_need(residual, "residual", x.dtype, (*lead, D)))
+            out["residual"] = residual_out
+        if residual_out is not None:
+            a.residual_out = _ptr(_need(residual_out, "residual_out", x.dtype, (*lead, D)))
+        _check(lib().ssdi8_norm_quantize(M, D, int(groups), ctypes.byref(a), _stream(stream)),
+               "ssdi8_norm_quantize")
+    return out
+
+
+def quantize_mx(x: torch.Tensor, format: str = "mxfp4", *, stream=None) -> Mx:
+    """Rows (..., K) in blocks of 32 that share a power of two (ssdi8_quantize_mx): x fp32, fp16 or bf16, its rows at
+    one stride; format "mxfp4" or "mxfp8"."""
+    fmt = _format(format, ("mxfp8", "mxfp4"))
+    if stream is None and _here(x):
+        r = _native.quantize_mx(x, fmt, _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_quantize_mx")
+            return Mx(r[1], r[2])
+    with _device_of(x, stream):
+        lead = tuple(x.shape[:-1])
+        xr = _flat(x, "x")
+        _activation_type(xr, "x", 2)
+        M, K = xr.shape
+        _rows(xr, "x", x.dtype, (M, K))
+        codes, scales, stype = _code_shapes(lead, K, format)
+        with _on(stream):
+            out = Mx(torch.empty(codes, dtype=_CODES[format], device=x.device),
+                     torch.empty(scales, dtype=stype, device=x.device))
+        _check(lib().ssdi8_quantize_mx(M, K, _ptr(xr), _DTYPES[x.dtype], xr.stride(0), fmt,
+                                       _ptr(out.codes), _ptr(out.scales), _stream(stream)),
+               "ssdi8_quantize_mx")
+    return out
+
+
+def _mx(t, name: str):
+    """(format, rows' shape, values of a row) of an Mx."""
+    codes, scales = t
+    if codes.dtype not in (torch.uint8, torch.float8_e4m3fn):
+        raise ValueError(f"{name}: codes must be torch.uint8 or torch.float8_e4m3fn, got {codes.dtype}")
+    if codes.dim() < 2:
+        raise ValueError(f"{name}: codes must be rows")
+    format = "mxfp4" if codes.dtype == torch.uint8 else "mxfp8"
+    lead, k = tuple(codes.shape[:-1]), codes.shape[-1] * (2 if format == "mxfp4" else 1)
+    if k % MX_BLOCK:
+        raise ValueError(f"{name}: {k} values of a row are no whole blocks of {MX_BLOCK}")
+    _need(codes, f"{name}: codes")
+    _need(scales, f"{name}: scales", torch.float8_e8m0fnu, (*lead, k // MX_BLOCK))
+    return format, lead, k
+
+
+def linear_mx(x: Union[Mx, torch.Tensor], weight: Mx, *, x_format: str = "mxfp8",
+              bias: Optional[torch.Tensor] = None, activation: Optional[str] = None,
+              residual: Optional[torch.Tensor] = None, y_dtype: Optional[torch.dtype] = None,
+              y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """A projection with weights in microscaled 4-bit floating point and its epilogue (ssdi8_linear_mx):
+    act(x weight^T + bias) + residual.  weight: Mx of (O, K) in "mxfp4"; x: Mx of (..., K), or a tensor (..., K), which
+    is brought to x_format ("mxfp8" or "mxfp4") first; bias (O) fp32, activation None, "silu", "gelu" or
+    "softplus", residual (..., O) of y's type.  y (..., O) is y_dtype: fp32, fp16 or bf16 (of a tensor x, unless
+    given, x's type; else fp16)."""
+    _format(x_format, ("mxfp8", "mxfp4"))
+    if isinstance(x, torch.Tensor):
+        if y is None and y_dtype is None:
+            y_dtype = x.dtype
+        if not isinstance(weight, tuple) or len(weight) != 2:
+            raise ValueError("weight must be an Mx")
+        if x.dim() < 2 or -(-x.shape[-1] // MX_BLOCK) != weight[1].shape[-1]:
+            raise ValueError(f"x must be rows of the weight's {weight[1].shape[-1]} blocks of {MX_BLOCK}")
+        x = quantize_mx(x, x_format, stream=stream)
+    if y is None and stream is None and activation in ACT and (y_dtype is None or y_dtype in _DTYPES) \
+            and isinstance(x, tuple) and isinstance(weight, tuple) and len(x) == len(weight) == 2 and _here(x[0]):
+        r = _native.linear_mx(x[0], x[1], weight[0], weight[1], bias, ACT[activation], residual,
+                              F16 if y_dtype is None else _DTYPES[y_dtype], _raw_stream(None))
+        if r is not None:
+            if r[0] != OK:
+                _check(r[0], "ssdi8_linear_mx")
+            return r[1]
+    if not isinstance(x, tuple) or len(x) != 2 or not isinstance(weight, tuple) or len(weight) != 2:
+        raise ValueError("x must be an Mx or a tensor, weight an Mx")
+    with _device_of(x[0], stream, x[1], *weight, bias, residual, y):
+        format, lead, k = _mx(x, "x")
+        wformat, (O, *more), wk = _mx(weight, "weight")
+        if wformat != "mxfp4" or more:
+            raise ValueError("weight must be (outputs, inputs) in mxfp4")
+        if wk != k:
+            raise ValueError(f"x has {k} values in a row, weight {wk}")
+        a = LinearMxArgs()
+        a.x_format = FORMAT[format]
+        a.x_codes, a.x_scales, a.weight_codes, a.weight_scales = (_ptr(t) for t in (*x, *weight))
+        a.bias = _param(bias, "bias", (O,))
+        a.act = _act(activation, (0, 1, 2, 3))
+        y_dtype = (torch.float16 if y is None else y.dtype) if y_dtype is None else y_dtype
+        if y_dtype not in _ACTIVATIONS:
+            raise ValueError(f"unsupported y_dtype {y_dtype}")
+        if y is None:
+            with _on(stream):
+                y = torch.empty(*lead, O, dtype=y_dtype, device=x[0].device)
+        M = x[0].numel() // max(1, x[0].shape[-1])
+        yr = _rows(_flat(y, "y"), "y", y_dtype, (M, O))
+        if tuple(y.shape) != (*lead, O):
+            raise ValueError(f"y must have shape {(*lead, O)}, got {tuple(y.shape)}")
+        a.y, a.y_row_stride, a.y_dtype = _ptr(yr), max(yr.stride(0), O) if M <= 1 else yr.stride(0), _DTYPES[y_dtype]
+        if residual is not None:
+            if tuple(residual.shape) != (*lead, O):
+                raise ValueError(f"residual must have shape {(*lead, O)}, got {tuple(residual.shape)}")
+            rr = _rows(_flat(residual, "residual"), "residual", y_dtype, (M, O))
+            a.residual, a.residual_row_stride = _ptr(rr), rr.stride(0)
+        _check(lib().ssdi8_linear_mx(M, O, k, ctypes.byref(a), _stream(stream)), "ssdi8_linear_mx")
     return y
 
 
