@@ -48,15 +48,34 @@ template <typename T> __device__ __forceinline__ v4f mma(const Frag<T>& a, const
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, a), __builtin_bit_cast(v8h, b), c, 0, 0, 0);
   }
 }
-// A value as the sum of two of the type (fp32: itself), in slot e of two fragments.
-template <typename T> __device__ __forceinline__ void split(float f, Frag<T>& hi, Frag<T>& lo, int e) {
-  hi.v[e] = (T)f;
-  if constexpr (sizeof(T) == 2) lo.v[e] = (T)(f - (float)hi.v[e]);
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef bf16 v2b __attribute__((ext_vector_type(2)));
+template <typename T> struct TwoOf { typedef v2h type; };
+template <> struct TwoOf<bf16> { typedef v2b type; };
+
+// Eight values as a fragment, rounded to the type.
+template <typename T> __device__ __forceinline__ Frag<T> round_frag(const float (&f)[8]) {
+  Frag<T> r;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r.v[e] = f[e];
+  } else {
+    typedef typename TwoOf<T>::type Two;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+      const Two t = __builtin_convertvector(v2f{f[e], f[e + 1]}, Two);
+      __builtin_memcpy(&r.v[e], &t, 4);
+    }
+  }
+  return r;
 }
-template <typename T> __device__ __forceinline__ v4f mma_split(const Frag<T>& ahi, const Frag<T>& alo, const Frag<T>& b, v4f c) {
-  c = mma(ahi, b, c);
-  if constexpr (sizeof(T) == 2) c = mma(alo, b, c);
-  return c;
+// What that leaves of them, as a second fragment (16-bit types).
+template <typename T> __device__ __forceinline__ Frag<T> rest_frag(const float (&f)[8], const Frag<T>& hi) {
+  float d[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) d[e] = f[e] - (float)hi.v[e];
+  return round_frag<T>(d);
 }
 
 // The exponent shift that brings magnitude bits `big` of fp32 to [2^14, 2^15); 0 for 0 and for what is no number.
@@ -71,38 +90,53 @@ __device__ __forceinline__ uint32_t bits_max(uint32_t a, float v) {
   const uint32_t m = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
   return a > m ? a : m;
 }
-__device__ __forceinline__ uint32_t group_max(uint32_t v) {   // over the four lane groups
-#pragma unroll
-  for (int d = 16; d < 64; d *= 2) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)v, d);
-    v = v > o ? v : o;
-  }
-  return v;
+// The largest over the four lane groups, and over all lanes, in each of them.
+__device__ __forceinline__ uint32_t group_max(uint32_t v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  v = a[0] > a[1] ? a[0] : a[1];
+  const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  return b[0] > b[1] ? b[0] : b[1];
+}
+template <int kCtrl> __device__ __forceinline__ uint32_t lane_max(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xf, 0xf, true);
+  return v > o ? v : o;
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  return group_max(lane_max<0x140>(lane_max<0x141>(lane_max<0x4E>(lane_max<0xB1>(v)))));
+}
+// Sums over the lanes up to each.
+__device__ __forceinline__ double wave_scan(double v) {
+  v = dpp_add_f64<0x111, 0xf>(v);   // 1, 2, 4 and 8 lanes to the left within 16
+  v = dpp_add_f64<0x112, 0xf>(v);
+  v = dpp_add_f64<0x114, 0xf>(v);
+  v = dpp_add_f64<0x118, 0xf>(v);
+  v = dpp_add_f64<0x142, 0xa>(v);   // the last lane of a row of 16 into the next row, of 32 into the next half
+  return dpp_add_f64<0x143, 0xc>(v);
 }
 
-// Two times four values: places [at, at + 4) and [at + 16, at + 20) of an LDS row.
+// Eight values of an LDS row.
 template <typename T> __device__ __forceinline__ Frag<T> row_frag(const T* p) {
   Frag<T> f;
-  __builtin_memcpy(&f.v[0], __builtin_assume_aligned(p, 4 * sizeof(T)), 4 * sizeof(T));
-  __builtin_memcpy(&f.v[4], __builtin_assume_aligned(p + 16, 4 * sizeof(T)), 4 * sizeof(T));
+  __builtin_memcpy(&f, __builtin_assume_aligned(p, 16), sizeof(f));
   return f;
 }
-// The same of a column: rows [4 g, 4 g + 4) and 16 further on, of 16 columns at p (p: row 0 of the 32, LDS).
-template <typename T, int kStride> __device__ __forceinline__ Frag<T> column_frag(const T* p, int lane) {
+// Of 16 columns of 32 LDS rows the lane's column, rows [4 g, 4 g + 4) and 16 further on.  at(row, c): where values
+// 4 c .. 4 c + 3 of a row's 16 columns are.
+template <typename T, typename At> __device__ __forceinline__ Frag<T> column_frag(const T* p, int lane, At at) {
   Frag<T> f;
   const int g = lane >> 4, m = lane & 15;
   if constexpr (sizeof(T) == 2) {
     // the four values that lane m of a group points at are a quarter of row m / 4 of a 4 x 16 block, which the
     // instruction hands out by columns
     typedef __attribute__((address_space(3))) v4s* Lds;
-    T* q = const_cast<T*>(p) + (4 * g + m / 4) * kStride + 4 * (m % 4);
-    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(q));
-    const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(q + 16 * kStride));
+    T* q = const_cast<T*>(p);
+    const v4s a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(q + at(4 * g + m / 4, m % 4)));
+    const v4s b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(q + at(16 + 4 * g + m / 4, m % 4)));
     __builtin_memcpy(&f.v[0], &a, 8);
     __builtin_memcpy(&f.v[4], &b, 8);
   } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f.v[e] = p[(4 * g + e % 4 + e / 4 * 16) * kStride + m];
+    for (int e = 0; e < 8; ++e) f.v[e] = p[at(4 * g + e % 4 + e / 4 * 16, m / 4) + m % 4];
   }
   return f;
 }
@@ -110,80 +144,140 @@ template <typename T, int kStride> __device__ __forceinline__ Frag<T> column_fra
 struct Args {
   LinearAttention a;
   int slices, spans, chunks, span_chunks;   // column slices of a head; spans of the tokens and their chunks
+  int groups;                               // of heads: those that a workgroup takes together
 };
 
-// Floats of a head's state in the workspace, and where the spans' decays lie behind the states.
 __device__ __host__ __forceinline__ int64_t state_floats(const LinearAttention& a) { return a.keys * a.values; }
 
-// A tile of rows on its way from memory to LDS: kRows rows of kWidth values (`width` of them there), by 256 threads
-// in vectors of 16 bytes.
-template <typename T, int kRows, int kWidth> struct Stage {
-  static constexpr int kPer = 16 / (int)sizeof(T), kVecs = kWidth / kPer;
-  static constexpr int kEach = (kRows * kVecs + 255) / 256;
-  static_assert(kRows * kVecs % 256 == 0 || kEach == 1, "stage");
+// Memory from p on for loads and stores with offsets of less than 2^31 bytes; at kNowhere loads give 0 and stores do
+// nothing, so that what is not there needs no branch.
+constexpr uint32_t kNowhere = 0xfffffff0u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x80000000u, 0x00027000);
+}
+
+// A tile of rows on its way from memory to LDS: kRows rows of kWidth values (`width` of every kPart there, the parts
+// `part` elements apart), by 256 threads in vectors of 16 bytes.  Offsets within the tile are of 32 bits (the host
+// refuses tokens too far apart for them).
+template <typename T, int kRows, int kWidth, int kPart> struct Stage {
+  static constexpr int kPer = 16 / (int)sizeof(T), kVecs = kWidth / kPer, kStep = 256 / kVecs;
+  static constexpr int kEach = kRows / kStep;
+  static_assert(kRows % kStep == 0 && 256 % kVecs == 0 && kPart % kPer == 0, "stage");
   uint4 v[kEach];
-  __device__ __forceinline__ void load(const T* base, int64_t token_stride, int tokens, int width, int tid) {
+  static __device__ __forceinline__ int column(int tid) { return tid % kVecs * kPer; }
+  static __device__ __forceinline__ uint32_t offset(int64_t token_stride, int64_t part, int tid) {
+    const int c = column(tid);
+    return (uint32_t)((tid / kVecs * token_stride + (kPart < kWidth ? c / kPart * part : 0) + c % kPart) * sizeof(T));
+  }
+  __device__ __forceinline__ void load(const T* base, uint32_t off, int64_t token_stride, int tokens, int width, int tid) {
+    const int in = column(tid) % kPart, row0 = tid / kVecs;
+    const auto tile = buffer_of(base);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int at = i * 256 + tid, row = at / kVecs, c = at % kVecs * kPer;
-      v[i] = make_uint4(0, 0, 0, 0);
-      if (row >= tokens || row >= kRows) continue;
-      const T* p = base + row * token_stride + c;
-      if (c + kPer <= width) {
-        __builtin_memcpy(&v[i], p, 16);
-      } else {
-        T e[kPer];
+      const uint32_t at = i * kStep + row0 < tokens && in + kPer <= width ? off : kNowhere;
+      const auto d = __builtin_amdgcn_raw_buffer_load_b128(tile, (int)at, (int)(i * kStep * token_stride * sizeof(T)), 0);
+      v[i] = __builtin_bit_cast(uint4, d);
+    }
+    if (width % kPer == 0) return;
+    // the row's last vector, value by value
+    if (in >= width || in + kPer <= width) return;
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) e[j] = c + j < width ? p[j] : (T)0.0f;
-        __builtin_memcpy(&v[i], e, 16);
+    for (int i = 0; i < kEach; ++i) {
+      if (i * kStep + row0 >= tokens) continue;
+      const T* p = reinterpret_cast<const T*>(reinterpret_cast<const char*>(base + i * kStep * token_stride) + off);
+      uint64_t half[2] = {0, 0};
+#pragma unroll 1
+      for (int j = 0; j < width - in; ++j) {
+        uint64_t e = 0;
+        __builtin_memcpy(&e, p + j, sizeof(T));
+        const uint64_t at = e << (8 * sizeof(T) * (j % (kPer / 2)));
+        half[0] |= j < kPer / 2 ? at : 0;
+        half[1] |= j < kPer / 2 ? 0 : at;
       }
+      __builtin_memcpy(&v[i], half, 16);
     }
   }
-  __device__ __forceinline__ void put(T* lds, int stride, int tid) const {
+  template <typename At> __device__ __forceinline__ void put(T* lds, int tid, At at) const {   // at(row, column)
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int at = i * 256 + tid, row = at / kVecs, c = at % kVecs * kPer;
-      if (row < kRows) *reinterpret_cast<uint4*>(lds + row * stride + c) = v[i];
-    }
+    for (int i = 0; i < kEach; ++i)
+      *reinterpret_cast<uint4*>(lds + at(i * kStep + tid / kVecs, column(tid))) = v[i];
   }
 };
 
-// kKeys: keys filled up to 64, 128 or 256.  kTiles: tiles of 16 columns per wave.  kC: tokens of a chunk.
-// kOut: the walk with outputs; else the one for the states at the spans' ends.
-template <typename T, int kKeys, int kTiles, int kC, bool kOut>
-__global__ __launch_bounds__(256) void attention_kernel(Args p) {
-  const LinearAttention& a = p.a;
-  constexpr int kSlice = 64 * kTiles;                       // columns of a workgroup
-  constexpr int kSums = kC / 32, kRowsT = kC / 16, kKeyT = kKeys / 16, kKeyS = kKeys / 32;
-  constexpr int kPad = 16 / (int)sizeof(T);
-  constexpr int kQ = kKeys + kPad, kV = kSlice + kPad;      // LDS row lengths
-  constexpr int kHalves = sizeof(T) == 2 ? 2 : 1;
-  __shared__ __attribute__((aligned(16))) T q_lds[kOut ? kC * kQ : 8];
-  __shared__ __attribute__((aligned(16))) T k_lds[kC * kQ];
-  __shared__ __attribute__((aligned(16))) T v_lds[kC * kV];
-  __shared__ __attribute__((aligned(16))) Frag<T> p_lds[kOut ? kRowsT * kSums * kHalves * 64 : 1];
-  __shared__ double c_lds[kC];
-  __shared__ float row_scale[kC];
+// The magnitude bits of a fragment's largest value (as those of the type), 16-bit types.
+__device__ __forceinline__ uint32_t pk_max_u16(uint32_t a, uint32_t b) {
+  typedef unsigned short v2u __attribute__((ext_vector_type(2)));
+  const v2u x = __builtin_bit_cast(v2u, a), y = __builtin_bit_cast(v2u, b);
+  return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(x, y));
+}
+template <typename T> __device__ __forceinline__ uint32_t largest(const Frag<T>& f, uint32_t big) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) big = bits_max(big, f.v[e]);
+  } else {
+    uint32_t w[4];
+    __builtin_memcpy(w, f.v, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) big = pk_max_u16(big, w[i] & 0x7fff7fffu);
+  }
+  return big;
+}
 
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, m = lane & 15;
+// kKeys: keys filled up to 64, 128 or 256.  kHeads (1 or 2) heads of y that share q and k, each with 4 / kHeads waves of
+// kTiles tiles of 16 columns.  kC: tokens of a chunk.  kOut: the walk with outputs; else the one for the states at
+// the spans' ends.
+template <typename T, int kKeys, int kTiles, int kHeads, int kC, bool kOut>
+__global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Args p) {
+  const LinearAttention& a = p.a;
+  constexpr bool kHalf = sizeof(T) == 2, kF16 = std::is_same_v<T, _Float16>;
+  constexpr int kWH = 4 / kHeads, kSlice = 16 * kTiles * kWH;   // waves of a head, its columns in a workgroup
+  constexpr int kSums = kC / 32, kRowsT = kC / 16, kKeyT = kKeys / 16, kKeyS = kKeys / 32;
+  // LDS row lengths.  q is read by rows, 16 bytes of 16 rows at a time: 4 banks from row to row; v by four rows of 32
+  // bytes: 8 banks.  k is read both ways: its rows' chunks of 16 bytes are exchanged (k_at), so that 16 rows at one
+  // chunk, and four rows at four chunks, lie in different banks.
+  constexpr int kPerChunk = 16 / (int)sizeof(T);
+  constexpr int kQ = kKeys + kPerChunk, kV = kSlice * kHeads + 2 * kPerChunk;
+  auto q_at = [](int row, int key) { return row * kQ + key; };
+  auto v_at = [](int row, int col) { return row * kV + col; };
+  auto k_at = [](int row, int key) {
+    constexpr int kChunks = kKeys / kPerChunk;
+    const int f = kChunks >= 16 ? row % 4 * 4 + row / 4 % 4 : row / 2 % 2 * 4 + row / 4 % 4;
+    // fp32: whole pairs of chunks
+    return row * kKeys + ((key / kPerChunk) ^ (kHalf ? f : 2 * f % 16)) * kPerChunk + key % kPerChunk;
+  };
+  constexpr int kPairs = kRowsT * (kRowsT / 2 + 1) / 2;     // (row tile, 32 tokens) of p that are not 0
+  constexpr int kOutSize = kC * kSlice * kHeads;             // of y's tile, which takes the place of q
+  __shared__ __attribute__((aligned(16))) T q_lds[kOut ? (kC * kQ > kOutSize ? kC * kQ : kOutSize) : 8];
+  __shared__ __attribute__((aligned(16))) T k_lds[kC * kKeys];
+  __shared__ __attribute__((aligned(16))) T v_lds[kC * kV];
+  __shared__ __attribute__((aligned(16))) Frag<T> p_lds[kHeads][kOut ? kPairs * 64 : 1];
+  __shared__ __attribute__((aligned(16))) double c_all[kHeads][kC];
+  __shared__ __attribute__((aligned(16))) float w_all[kHeads][kC], e_all[kHeads][kC], row_all[kHeads][kC];
+  __shared__ __attribute__((aligned(16))) float b_all[kHeads][kWH][kC];
+
+  const int tid = threadIdx.x, lane = tid & 63, lane_g = lane >> 4, lane_m = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // the same in all lanes: branches by it are scalar
+  const int sub = kHeads > 1 ? wave / kWH : 0, hw = wave % kWH;   // head of the workgroup, wave of the head
+  double* c_lds = c_all[sub];
+  float *w_lds = w_all[sub], *e_lds = e_all[sub], *row_scale = row_all[sub], *b_lds = b_all[sub][hw];
   int id = xcd_remap(blockIdx.x, gridDim.x);
   const int slice = id % p.slices;
   id /= p.slices;
   // heads are neighbours: those that share q and k share an XCD's cache
   const int heads = (int)(kOut ? a.heads : a.v_heads);
-  const int h = id % heads;
-  id /= heads;
+  const int h0 = id % p.groups * kHeads, h = h0 + sub;
+  id /= p.groups;
   const int span = id % (kOut ? p.spans : p.spans - 1);
   const int64_t b = id / (kOut ? p.spans : p.spans - 1);
-  const int hq = (int)(h * a.q_heads / heads), hv = (int)(h * a.v_heads / heads);
-  const int hk = (int)(hv * a.k_heads / a.v_heads);
+  const int hq = (int)(h0 * a.q_heads / heads), hv0 = (int)(h0 * a.v_heads / heads), hv = hv0 + sub;
+  const int hk = (int)(hv0 * a.k_heads / a.v_heads);
   const int col0 = slice * kSlice;
   const int cols = (int)(a.values - col0 < kSlice ? a.values - col0 : kSlice);
   const int keys = (int)a.keys;
 
   const T* qp = static_cast<const T*>(a.q) + b * a.qs.batch + hq * a.qs.head;
   const T* kp = static_cast<const T*>(a.k) + b * a.ks.batch + hk * a.ks.head;
-  const T* vp = static_cast<const T*>(a.v) + b * a.vs.batch + hv * a.vs.head + col0;
+  const T* vp = static_cast<const T*>(a.v) + b * a.vs.batch + hv0 * a.vs.head + col0;
   int64_t end = a.seqlen;
   if (a.lengths) {
     const int64_t n = a.lengths[b];
@@ -194,8 +288,10 @@ __global__ __launch_bounds__(256) void attention_kernel(Args p) {
   const int live = (int)((end + kC - 1) / kC);               // chunks with tokens
   const int last = live < chunk1 ? live : chunk1;
 
-  // the state: rows 16 t + 4 g + (0..3) of key tile t, column m of column tile n
-  const int my0 = wave * kTiles * 16;
+  // The state: keys key_of(t, g) + (0..3) of key tile t, column m of column tile n.  The keys of two tiles are dealt
+  // out so that a lane's eight rows of them are eight neighbouring keys: those of its part of q.
+  auto key_of = [](int t, int quarter) { return t / 2 * 32 + 8 * quarter + t % 2 * 4; };
+  const int my0 = hw * kTiles * 16;
   const int64_t states = a.batch * a.v_heads * state_floats(a);
   v4f S[kKeyT][kTiles];
   {
@@ -205,24 +301,36 @@ __global__ __launch_bounds__(256) void attention_kernel(Args p) {
 #pragma unroll
     for (int t = 0; t < kKeyT; ++t)
 #pragma unroll
-      for (int n = 0; n < kTiles; ++n)
+      for (int n = 0; n < kTiles; ++n) S[t][n] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    if (from) {
+      from += col0 + my0;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int key = 16 * t + 4 * g + r, col = my0 + 16 * n + m;
-          S[t][n][r] = from && key < keys && col < cols ? from[(int64_t)key * a.values + col0 + col] : 0.0f;
+      for (int n = 0; n < kTiles; ++n)
+        if (my0 + 16 * n + lane_m < cols) {
+#pragma unroll
+          for (int t = 0; t < kKeyT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (key_of(t, lane_g) + r < keys)
+                S[t][n][r] = from[(int64_t)(key_of(t, lane_g) + r) * a.values + 16 * n + lane_m];
         }
+    }
   }
   double total = 0.0;   // of the decays' logarithms (base 2) over the span
 
-  Stage<T, kC, kKeys> q_next, k_next;
-  Stage<T, kC, kSlice> v_next;
+  typedef Stage<T, kC, kKeys, kKeys> KeyStage;
+  typedef Stage<T, kC, kSlice * kHeads, kSlice> ValueStage;
+  KeyStage q_next, k_next;
+  ValueStage v_next;
+  const uint32_t q_off = KeyStage::offset(a.qs.token, 0, tid), k_off = KeyStage::offset(a.ks.token, 0, tid);
+  const uint32_t v_off = ValueStage::offset(a.vs.token, a.vs.head, tid);
   float g_next = 0.0f;
   auto request = [&](int chunk) {
     const int64_t t0 = (int64_t)chunk * kC;
     const int tokens = (int)(end - t0 < kC ? end - t0 : kC);
-    if constexpr (kOut) q_next.load(qp + t0 * a.qs.token, a.qs.token, tokens, keys, tid);
-    k_next.load(kp + t0 * a.ks.token, a.ks.token, tokens, keys, tid);
-    v_next.load(vp + t0 * a.vs.token, a.vs.token, tokens, cols, tid);
+    if constexpr (kOut) q_next.load(qp + t0 * a.qs.token, q_off, a.qs.token, tokens, keys, tid);
+    k_next.load(kp + t0 * a.ks.token, k_off, a.ks.token, tokens, keys, tid);
+    v_next.load(vp + t0 * a.vs.token, v_off, a.vs.token, tokens, cols, tid);
     g_next = 0.0f;
     if (a.log_decay && lane < tokens)
       g_next = a.token_decay ? a.log_decay[b * a.g_batch + (t0 + lane) * a.g_token + hv] : a.log_decay[hv];
@@ -230,84 +338,158 @@ __global__ __launch_bounds__(256) void attention_kernel(Args p) {
 
   if (chunk0 < last) request(chunk0);
   for (int chunk = chunk0; chunk < last; ++chunk) {
+    // The lane's places are formed anew for every chunk: kept over all of them, places and constants took up so many
+    // registers that 50 went to memory, where their way back waits for the loads in flight.
+    int g = lane_g, m = lane_m;
+    asm volatile("" : "+v"(g), "+v"(m));
+    const int lane = g * 16 + m;
     __syncthreads();   // the last chunk is read
-    if constexpr (kOut) q_next.put(q_lds, kQ, tid);
-    k_next.put(k_lds, kQ, tid);
-    v_next.put(v_lds, kV, tid);
-    // sums of the decays' logarithms, in base 2; below 2^-100000 is 0 all the same, and an infinite one would leave
+    if constexpr (kOut) q_next.put(q_lds, tid, q_at);
+    k_next.put(k_lds, tid, k_at);
+    v_next.put(v_lds, tid, v_at);
+    // sums of the decays' logarithms, in base 2; below 2^-65536 is 0 all the same, and an infinite one would leave
     // no differences behind it
     double c = g_next < -65536.0f ? -65536.0 * kLog2e : (double)g_next * kLog2e;
-#pragma unroll
-    for (int d = 1; d < kC; d *= 2) {
-      const double o = __shfl_up(c, d);
-      c = lane >= d ? c + o : c;
-    }
-    if (wave == 0 && lane < kC) c_lds[lane] = c;
+    c = wave_scan(c);
     const double c_end = __shfl(c, kC - 1);
+    if (hw == 0 && lane < kC) {
+      c_lds[lane] = c;
+      w_lds[lane] = __builtin_amdgcn_exp2f((float)(c_end - c));
+      if constexpr (kOut) e_lds[lane] = a.scale * __builtin_amdgcn_exp2f((float)c);
+    }
     __syncthreads();
-    if (chunk + 1 < last) request(chunk + 1);
 
     const int64_t t0 = (int64_t)chunk * kC;
     if constexpr (kOut) {
-      // p^T: rows j, column i = m of row tile `wave`
-      for (int it = wave; it < kRowsT; it += 4) {
+      // p^T: rows j, column i = m of row tile it; the waves of a head take one from each end of them in turn
+#pragma unroll
+      for (int u = 0; u < (kRowsT + kWH - 1) / kWH; ++u) {
+        const int it = u % 2 == 0 ? u * kWH + hw : (u + 1) * kWH - 1 - hw;
+        if (it >= kRowsT) continue;
         const int i = it * 16 + m;
-        const double ci = c_lds[i];
+        constexpr int kAll = kRowsT;
+        const int most = (u + 1) * kWH < kAll ? (u + 1) * kWH : kAll;   // tiles that any wave has in this turn
         v4f acc[kRowsT] = {};
 #pragma unroll
         for (int s = 0; s < kKeyS; ++s) {
-          const Frag<T> qf = row_frag(q_lds + i * kQ + 32 * s + 4 * g);
+          const Frag<T> qf = row_frag(q_lds + q_at(i, 32 * s + 8 * g));
 #pragma unroll
           for (int jt = 0; jt < kRowsT; ++jt)
-            if (jt <= it) acc[jt] = mma(row_frag(k_lds + (jt * 16 + m) * kQ + 32 * s + 4 * g), qf, acc[jt]);
+            if (jt < most) acc[jt] = mma(row_frag(k_lds + k_at(jt * 16 + m, 32 * s + 8 * g)), qf, acc[jt]);
         }
-        uint32_t big = 0;
+        // exp(c_i - c_j) for tokens j of earlier row tiles is exp(c_i - c_x) exp(c_x - c_j), x the last of them: both
+        // at most 1, the second one for all rows
+        const double ci = c_lds[i], cx = c_lds[it > 0 ? it * 16 - 1 : 0];
+        if (lane < kC) b_lds[lane] = __builtin_amdgcn_exp2f((float)(cx - c_lds[lane]));
+        const float ai = a.scale * __builtin_amdgcn_exp2f((float)(ci - cx));
+        double cj[4];
 #pragma unroll
-        for (int jt = 0; jt < kRowsT; ++jt)
+        for (int r = 0; r < 4; ++r) cj[r] = c_lds[it * 16 + 4 * g + r];
+        float wd[4];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const int j = jt * 16 + 4 * g + r;
-            const float w = a.scale * __builtin_amdgcn_exp2f((float)(ci - c_lds[j]));
-            acc[jt][r] = j <= i ? acc[jt][r] * w : 0.0f;
-            big = bits_max(big, acc[jt][r]);
+        for (int r = 0; r < 4; ++r) wd[r] = a.scale * __builtin_amdgcn_exp2f((float)(ci - cj[r]));
+        __builtin_amdgcn_wave_barrier();
+        float big = 0.0f;
+#pragma unroll
+        for (int jt = 0; jt < kRowsT; ++jt) {
+          if (jt >= most) continue;
+          if (jt < it) {
+            const float4 bj = *reinterpret_cast<const float4*>(b_lds + jt * 16 + 4 * g);
+            acc[jt][0] *= bj.x * ai;
+            acc[jt][1] *= bj.y * ai;
+            acc[jt][2] *= bj.z * ai;
+            acc[jt][3] *= bj.w * ai;
+          } else {   // tokens behind the row are left out
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float v = acc[jt][r] * wd[r];
+              acc[jt][r] = jt == it && 4 * g + r <= m ? v : 0.0f;
+            }
           }
-        float up = 1.0f;
-        if constexpr (std::is_same_v<T, _Float16>) {
-          const int s = range_shift(group_max(big));
-          up = power(s);
-          if (g == 0) row_scale[i] = power(-s);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) big = __builtin_fmaxf(big, __builtin_fabsf(acc[jt][r]));
         }
+        float up = 1.0f;
+        if constexpr (kF16) {
+          const int s = range_shift(group_max(__builtin_bit_cast(uint32_t, big)));
+          up = power(s);
+          if (g == 0) row_scale[i] = up;
+        }
+        const int pair0 = it / 2 * (it / 2 + 1) + it % 2 * (it / 2 + 1);
 #pragma unroll
         for (int s = 0; s < kSums; ++s) {
-          Frag<T> hi, lo;
+          if (2 * s > it) continue;
+          float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) split(acc[2 * s + e / 4][e % 4] * up, hi, lo, e);
-          p_lds[((it * kSums + s) * kHalves) * 64 + lane] = hi;
-          if constexpr (kHalves == 2) p_lds[((it * kSums + s) * kHalves + 1) * 64 + lane] = lo;
+          for (int e = 0; e < 8; ++e) f[e] = kF16 ? acc[2 * s + e / 4][e % 4] * up : acc[2 * s + e / 4][e % 4];
+          p_lds[sub][(pair0 + s) * 64 + lane] = round_frag<T>(f);
         }
       }
-      __syncthreads();
     }
 
-    // v as it is (for p v) and times exp(c_end - c_j) (for the state), where its values are no numbers 0
-    Frag<T> vf[kSums][kTiles], whi[kSums][kTiles], wlo[kSums][kTiles];
-    float down[kTiles];
+    v4f acc[kOut ? kRowsT : 1][kTiles] = {};
+    float s_down[kTiles];
+    if constexpr (kOut) {
+      // S^T q, the state rounded to the type
+      __builtin_amdgcn_sched_barrier(0);   // phases stay apart: their operands do not fit the registers together
+      float s_up[kTiles];
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) {
+        s_up[n] = s_down[n] = 1.0f;
+        if constexpr (kF16) {
+          float most = 0.0f;
+#pragma unroll
+          for (int t = 0; t < kKeyT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) most = __builtin_fmaxf(most, __builtin_fabsf(S[t][n][r]));
+          const int sh = range_shift(wave_max(__builtin_bit_cast(uint32_t, most)));
+          s_up[n] = power(sh);
+          s_down[n] = power(-sh);
+        }
+      }
+#pragma unroll
+      for (int s = 0; s < kKeyS; ++s) {
+        Frag<T> sf[kTiles];
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = kF16 ? S[2 * s + e / 4][n][e % 4] * s_up[n] : S[2 * s + e / 4][n][e % 4];
+          sf[n] = round_frag<T>(f);
+        }
+#pragma unroll
+        for (int it = 0; it < kRowsT; ++it) {
+          const Frag<T> qf = row_frag(q_lds + q_at(it * 16 + m, 32 * s + 8 * g));
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) acc[it][n] = mma(sf[n], qf, acc[it][n]);
+        }
+        if (s % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+      }
+      __syncthreads();   // p is there
+    }
+
+    // v, 0 where its values are no numbers
+    Frag<T> vf[kSums][kTiles];
+    uint32_t most_v[kTiles];
     int first[kTiles];   // the first token of the column whose value is no number
+    bool any_bad = false;
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      float w[kSums][8];
       uint32_t big = 0;
-      bool odd = false;
       first[n] = kC;
 #pragma unroll
       for (int s = 0; s < kSums; ++s) {
-        vf[s][n] = column_frag<T, kV>(v_lds + 32 * s * kV + my0 + 16 * n, lane);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) odd |= !(__builtin_fabsf((float)vf[s][n].v[e]) < __builtin_inff());
+        vf[s][n] = column_frag(v_lds + 32 * s * kV + sub * kSlice + my0 + 16 * n, lane,
+                               [&](int row, int c) { return v_at(row, 4 * c); });
+        big = largest(vf[s][n], big);
       }
+      if constexpr (kHalf) big = (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
+      const bool odd = big >= (kF16 ? 0x7c00u : kHalf ? 0x7f80u : 0x7f800000u);
       if (__any(odd)) {
+        any_bad = true;
+        big = 0;
 #pragma unroll
-        for (int s = 0; s < kSums; ++s)
+        for (int s = 0; s < kSums; ++s) {
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (!(__builtin_fabsf((float)vf[s][n].v[e]) < __builtin_inff())) {
@@ -315,124 +497,165 @@ __global__ __launch_bounds__(256) void attention_kernel(Args p) {
               first[n] = j < first[n] ? j : first[n];
               vf[s][n].v[e] = (T)0.0f;
             }
+          big = largest(vf[s][n], big);
+        }
+        if constexpr (kHalf) big = (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
 #pragma unroll
         for (int d = 16; d < 64; d *= 2) {
           const int o = __shfl_xor(first[n], d);
           first[n] = o < first[n] ? o : first[n];
         }
       }
-#pragma unroll
-      for (int s = 0; s < kSums; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int j = 32 * s + 16 * (e / 4) + 4 * g + e % 4;
-          w[s][e] = (float)vf[s][n].v[e] * __builtin_amdgcn_exp2f((float)(c_end - c_lds[j]));
-          big = bits_max(big, w[s][e]);
-        }
-      float up = 1.0f;
-      down[n] = 1.0f;
-      if constexpr (std::is_same_v<T, _Float16>) {
-        const int sh = range_shift(group_max(big));
-        up = power(sh);
-        down[n] = power(-sh);
-      }
-#pragma unroll
-      for (int s = 0; s < kSums; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) split(w[s][e] * up, whi[s][n], wlo[s][n], e);
+      most_v[n] = big;
     }
 
     if constexpr (kOut) {
-      const int64_t left = end - t0;
 #pragma unroll
-      for (int n = 0; n < kTiles; ++n) {
-        // the state as an operand
-        Frag<T> shi[kKeyS], slo[kKeyS];
-        float s_up = 1.0f, s_down = 1.0f;
-        if constexpr (std::is_same_v<T, _Float16>) {
-          uint32_t big = 0;
-#pragma unroll
-          for (int t = 0; t < kKeyT; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) big = bits_max(big, S[t][n][r]);
-#pragma unroll
-          for (int d = 1; d < 64; d *= 2) {
-            const uint32_t o = (uint32_t)__shfl_xor((int)big, d);
-            big = big > o ? big : o;
-          }
-          const int sh = range_shift(big);
-          s_up = power(sh);
-          s_down = power(-sh);
-        }
-#pragma unroll
-        for (int s = 0; s < kKeyS; ++s)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) split(S[2 * s + e / 4][n][e % 4] * s_up, shi[s], slo[s], e);
-        int bad[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) bad[r] = __shfl(first[n], 4 * g + r);
-#pragma unroll
-        for (int it = 0; it < kRowsT; ++it) {
-          const int i = it * 16 + m;
-          v4f before = {}, in = {};
-#pragma unroll
-          for (int s = 0; s < kKeyS; ++s)
-            before = mma_split(shi[s], slo[s], row_frag(q_lds + i * kQ + 32 * s + 4 * g), before);
-#pragma unroll
-          for (int s = 0; s < kSums; ++s)
-            if (2 * s <= it) {
-              const Frag<T>* at = p_lds + ((it * kSums + s) * kHalves) * 64 + lane;
-              in = mma(vf[s][n], at[0], in);
-              if constexpr (kHalves == 2) in = mma(vf[s][n], at[64], in);
-            }
-          const float e = a.scale * __builtin_amdgcn_exp2f((float)c_lds[i]) * s_down;
-          const float in_scale = std::is_same_v<T, _Float16> ? row_scale[i] : 1.0f;
-          float o[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            o[r] = __builtin_fmaf(before[r], e, in[r] * in_scale);
-            if (i >= bad[r]) o[r] = __builtin_nanf("");
-          }
-          const int col = my0 + 16 * n + 4 * g;
-          if (t0 + i < a.seqlen && col < cols) {
-            const bool dead = i >= left;   // behind the sequence's end: 0
-            T* y = static_cast<T*>(a.y) + ((b * a.seqlen + t0 + i) * a.heads + h) * a.values + col0 + col;
-            T out[4];
-#pragma unroll
-            for (int r = 0; r < 4; ++r) out[r] = (T)(dead ? 0.0f : o[r]);
-            if (col + 4 <= cols) {
-              __builtin_memcpy(y, out, sizeof(out));
-            } else {
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (col + r < cols) y[r] = out[r];
-            }
-          }
-        }
-      }
-    }
-
-    // the state behind the chunk
-    const float decay = __builtin_amdgcn_exp2f((float)c_end);
-#pragma unroll
-    for (int t = 0; t < kKeyT; ++t) {
-      v4f add[kTiles] = {};
-#pragma unroll
-      for (int s = 0; s < kSums; ++s) {
-        const Frag<T> kf = column_frag<T, kQ>(k_lds + 32 * s * kQ + 16 * t, lane);
+      for (int it = 0; it < kRowsT; ++it) {
+        const int i = it * 16 + m;
+        const float e = e_lds[i], in = kF16 ? row_scale[i] : 1.0f;
+        const float out = kF16 ? 1.0f / in : 1.0f;   // of a power of two: exact
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
-          add[n] = mma(kf, whi[s][n], add[n]);
-          if constexpr (kHalves == 2) add[n] = mma(kf, wlo[s][n], add[n]);
+          const float by = kF16 ? e * s_down[n] * in : e;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[it][n][r] *= by;
+        }
+        const int pair0 = it / 2 * (it / 2 + 1) + it % 2 * (it / 2 + 1);
+#pragma unroll
+        for (int s = 0; s < kSums; ++s)
+          if (2 * s <= it) {
+            const Frag<T> pf = p_lds[sub][(pair0 + s) * 64 + lane];
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) acc[it][n] = mma(vf[s][n], pf, acc[it][n]);
+          }
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[it][n][r] *= out;
+          if (any_bad) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+              if (i >= __shfl(first[n], 4 * g + r)) acc[it][n][r] = __builtin_nanf("");
+          }
         }
       }
+      __builtin_amdgcn_sched_barrier(0);
+      // y leaves through the place of q, which all waves have read: the wave's rows in whole vectors of 16 bytes.
+      // Chunk x of a row lies at x ^ (row / kPeriod): the 16 rows that are written at a time touch every bank once.
+      constexpr int kChunks = kTiles * (int)sizeof(T), kPeriod = 16 / kChunks, kPer = 16 / (int)sizeof(T);
+      char* out_lds = reinterpret_cast<char*>(q_lds) + wave * kC * kChunks * 16;
+      const int64_t left = end - t0;
+      if (left < kC) {   // tokens behind the sequence's end: 0
+#pragma unroll
+        for (int it = 0; it < kRowsT; ++it)
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[it][n][r] = it * 16 + m < left ? acc[it][n][r] : 0.0f;
+      }
+#pragma unroll
+      for (int it = 0; it < kRowsT; ++it)
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+          T v[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) v[r] = (T)acc[it][n][r];
+          const int i = it * 16 + m, x = (n * 16 + 4 * g) / kPer, in = (4 * g) % kPer * (int)sizeof(T);
+          __builtin_memcpy(__builtin_assume_aligned(out_lds + (i * kChunks + (x ^ (i / kPeriod % kChunks))) * 16 + in,
+                                                    4 * sizeof(T)), v, sizeof(v));
+        }
+      __builtin_amdgcn_wave_barrier();
+      const int rows = (int)(a.seqlen - t0 < kC ? a.seqlen - t0 : kC);
+      T* y = static_cast<T*>(a.y) + ((b * a.seqlen + t0) * a.heads + h) * a.values + col0 + my0;
+      const auto tile = buffer_of(y);
+      const int x = lane % kChunks, row0 = lane / kChunks, mine = cols - my0 - x * kPer;   // columns from mine on
+      const int y_row = (int)(a.heads * a.values);
+      const uint32_t y_off = (uint32_t)(row0 * y_row + x * kPer) * (uint32_t)sizeof(T);
+#pragma unroll
+      for (int u = 0; u < kC * kChunks / 64; ++u) {
+        const int row = u * (64 / kChunks) + row0;
+        typedef unsigned v4u __attribute__((ext_vector_type(4)));
+        const v4u v = *reinterpret_cast<const v4u*>(out_lds + (row * kChunks + (x ^ (row / kPeriod % kChunks))) * 16);
+        // The whole offset in the vector register: with a part of it in a scalar one the compiler leaves out the wait
+        // state between a store of 16 bytes and the next write to its data registers, and the hardware stored the
+        // first four bytes of some lanes from what was written there next.
+        const uint32_t step = (uint32_t)(u * (64 / kChunks) * y_row) * (uint32_t)sizeof(T);
+        const uint32_t at = row < rows && mine >= kPer ? y_off + step : kNowhere;
+        __builtin_amdgcn_raw_buffer_store_b128(v, tile, (int)at, 0, 0);
+      }
+      if (cols - my0 < 16 * kTiles && cols % kPer) {   // the rows' last vectors, value by value
+        if (mine > 0 && mine < kPer)
+#pragma unroll 1
+          for (int row = row0; row < rows; row += 64 / kChunks) {
+            const T* from = reinterpret_cast<const T*>(out_lds + (row * kChunks + (x ^ (row / kPeriod % kChunks))) * 16);
+#pragma unroll 1
+            for (int c = 0; c < mine; ++c) y[(int64_t)row * y_row + x * kPer + c] = from[c];
+          }
+      }
+    }
+    if (chunk + 1 < last) request(chunk + 1);
+
+    __builtin_amdgcn_sched_barrier(0);
+    // The state behind the chunk: v times exp(c_end - c_j), as two values of the type
+    const float decay = __builtin_amdgcn_exp2f((float)c_end);
+    float up[kTiles], down[kTiles];
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      up[n] = down[n] = 1.0f;
+      if constexpr (kF16) {
+        // as fp32's bits; the decays only make the values smaller
+        const float most = (float)__builtin_bit_cast(_Float16, (uint16_t)group_max(most_v[n]));
+        const int sh = range_shift(__builtin_bit_cast(uint32_t, most));
+        up[n] = power(sh);
+        down[n] = power(-sh);
+      }
+#pragma unroll
+      for (int t = 0; t < kKeyT; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) S[t][n][r] *= kF16 ? decay * up[n] : decay;
+    }
+#pragma unroll
+    for (int s = 0; s < kSums; ++s) {
+      Frag<T> whi[kTiles], wlo[kTiles];
+      const float4 wa = *reinterpret_cast<const float4*>(w_lds + 32 * s + 4 * g);
+      const float4 wb = *reinterpret_cast<const float4*>(w_lds + 32 * s + 16 + 4 * g);
+      const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) {
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * (kF16 ? w[e] * up[n] : w[e]);
+        whi[n] = round_frag<T>(f);
+        if constexpr (kHalf) wlo[n] = rest_frag(f, whi[n]);
+      }
+#pragma unroll
+      for (int t = 0; t < kKeyT; ++t) {
+        const Frag<T> kf = column_frag(k_lds, lane, [&](int row, int c) { return k_at(32 * s + row, key_of(t, c)); });
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n) {
+          S[t][n] = mma(kf, whi[n], S[t][n]);
+          if constexpr (kHalf) S[t][n] = mma(kf, wlo[n], S[t][n]);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (kF16) {
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          S[t][n][r] = __builtin_fmaf(S[t][n][r], decay, add[n][r] * down[n]);
-          if (first[n] < kC) S[t][n][r] = __builtin_nanf("");
-        }
+        for (int t = 0; t < kKeyT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) S[t][n][r] *= down[n];
+    }
+    if (any_bad) {
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n)
+        if (first[n] < kC)
+#pragma unroll
+          for (int t = 0; t < kKeyT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) S[t][n][r] = __builtin_nanf("");
     }
     total += c_end;
   }
@@ -440,7 +663,7 @@ __global__ __launch_bounds__(256) void attention_kernel(Args p) {
   if constexpr (kOut) {
     // tokens behind the last chunk with any
     for (int chunk = last > chunk0 ? last : chunk0; chunk < chunk1; ++chunk)
-      for (int o = tid; o < kC * kSlice; o += 256) {
+      for (int o = hw * 64 + lane; o < kC * kSlice; o += 64 * kWH) {
         const int64_t t = (int64_t)chunk * kC + o / kSlice;
         const int col = o % kSlice;
         if (t < a.seqlen && col < cols)
@@ -450,18 +673,21 @@ __global__ __launch_bounds__(256) void attention_kernel(Args p) {
   float* to = kOut ? (a.final_state && span == p.spans - 1 && h * a.v_heads % heads == 0 ? a.final_state : nullptr)
                    : a.workspace + span * states;
   if (to) {
-    to += (b * a.v_heads + hv) * state_floats(a);
+    to += (b * a.v_heads + hv) * state_floats(a) + col0 + my0;
+    // the places are formed anew: those of the first loads would stay in registers over all chunks
+    int group = lane_g, column = lane_m;
+    asm volatile("" : "+v"(group), "+v"(column));
 #pragma unroll
-    for (int t = 0; t < kKeyT; ++t)
+    for (int n = 0; n < kTiles; ++n)
+      if (my0 + 16 * n + column < cols) {
 #pragma unroll
-      for (int n = 0; n < kTiles; ++n)
+        for (int t = 0; t < kKeyT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int key = 16 * t + 4 * g + r, col = my0 + 16 * n + m;
-          if (key < keys && col < cols) to[(int64_t)key * a.values + col0 + col] = S[t][n][r];
-        }
+          for (int r = 0; r < 4; ++r)
+            if (key_of(t, group) + r < keys) to[(int64_t)(key_of(t, group) + r) * a.values + 16 * n + column] = S[t][n][r];
+      }
   }
-  if (!kOut && tid == 0 && slice == 0)
+  if (!kOut && hw == 0 && lane == 0 && slice == 0)
     (a.workspace + (p.spans - 1) * states)[(span * a.batch + b) * a.v_heads + hv] =
         __builtin_amdgcn_exp2f((float)total);
 }
@@ -580,17 +806,22 @@ __global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, 
 }
 
 int chunk_of(int dtype) { return dtype == SSDI8_F32 ? 32 : 64; }
-int tiles_of(int64_t values) { return values <= 64 ? 1 : 2; }
+
+// Two heads to a workgroup where they are narrow and share q and k.
+bool paired(const LinearAttention& a) {
+  return a.values <= 64 && a.keys <= 128 && a.heads == a.v_heads && a.heads / a.q_heads % 2 == 0 && a.heads / a.k_heads % 2 == 0;
+}
 
 Args plan(const LinearAttention& a) {
   Args p;
   p.a = a;
-  const int64_t c = chunk_of(a.dtype), slice = 64 * tiles_of(a.values);
+  const int64_t c = chunk_of(a.dtype), slice = a.values <= 64 || a.keys > 128 ? 64 : 128;
   p.slices = (int)((a.values + slice - 1) / slice);
   p.chunks = (int)((a.seqlen + c - 1) / c);
-  // Spans: two workgroups for every CU, each with four chunks at least.
-  const int64_t wgs = a.batch * a.heads * p.slices;
-  int64_t spans = wgs >= 256 || wgs == 0 ? 1 : (512 + wgs - 1) / wgs;
+  p.groups = (int)(paired(a) ? a.heads / 2 : a.heads);
+  // Spans: as many workgroups as the card holds at once (two for every CU), each with four chunks at least.
+  const int64_t wgs = a.batch * p.groups * p.slices, hold = a.keys > 128 ? 256 : 512;
+  int64_t spans = wgs == 0 ? 1 : hold / wgs;
   spans = spans < p.chunks / 4 ? spans : p.chunks / 4;
   if (spans < 1) spans = 1;
   p.span_chunks = (int)((p.chunks + spans - 1) / spans);
@@ -598,25 +829,35 @@ Args plan(const LinearAttention& a) {
   return p;
 }
 
-template <typename T, int kKeys, int kTiles> hipError_t run(const Args& p, hipStream_t st) {
+template <typename T, int kKeys, int kTiles, int kHeads> hipError_t run(const Args& p, hipStream_t st) {
   constexpr int kC = sizeof(T) == 4 ? 32 : 64;
   const LinearAttention& a = p.a;
   if (p.spans > 1) {
-    attention_kernel<T, kKeys, kTiles, kC, false>
-        <<<dim3((unsigned)(a.batch * a.v_heads * p.slices * (p.spans - 1))), 256, 0, st>>>(p);
+    Args s = p;
+    s.groups = (int)(a.v_heads / kHeads);
+    attention_kernel<T, kKeys, kTiles, kHeads, kC, false>
+        <<<dim3((unsigned)(a.batch * s.groups * p.slices * (p.spans - 1))), 256, 0, st>>>(s);
     const int64_t states = a.batch * a.v_heads * a.keys * a.values, wgs = (states + 255) / 256;
     attention_join_kernel<<<dim3((unsigned)(wgs < 4096 ? wgs : 4096)), 256, 0, st>>>(p);
   }
-  attention_kernel<T, kKeys, kTiles, kC, true>
-      <<<dim3((unsigned)(a.batch * a.heads * p.slices * p.spans)), 256, 0, st>>>(p);
+  attention_kernel<T, kKeys, kTiles, kHeads, kC, true>
+      <<<dim3((unsigned)(a.batch * p.groups * p.slices * p.spans)), 256, 0, st>>>(p);
   return hipGetLastError();
 }
 
+template <typename T, int kKeys> hipError_t by_values(const Args& p, hipStream_t st) {
+  if constexpr (kKeys > 128) {
+    return run<T, kKeys, 1, 1>(p, st);
+  } else {
+    if (p.a.values > 64) return run<T, kKeys, 2, 1>(p, st);
+    return paired(p.a) ? run<T, kKeys, 2, 2>(p, st) : run<T, kKeys, 1, 1>(p, st);
+  }
+}
+
 template <typename T> hipError_t by_size(const Args& p, hipStream_t st) {
-  const bool wide = tiles_of(p.a.values) == 2;
-  if (p.a.keys <= 64) return wide ? run<T, 64, 2>(p, st) : run<T, 64, 1>(p, st);
-  if (p.a.keys <= 128) return wide ? run<T, 128, 2>(p, st) : run<T, 128, 1>(p, st);
-  return wide ? run<T, 256, 2>(p, st) : run<T, 256, 1>(p, st);
+  if (p.a.keys <= 64) return by_values<T, 64>(p, st);
+  if (p.a.keys <= 128) return by_values<T, 128>(p, st);
+  return by_values<T, 256>(p, st);
 }
 
 template <typename T> hipError_t run_step(const LinearAttention& a, hipStream_t st) {

@@ -4,7 +4,9 @@ import torch
 
 from block_ref import HALF_ULP, TINY, U, assert_within, rounded, silu, silu_bound, softplus  # noqa: F401
 
-# What is left of a value that enters the matrix unit as the sum of two of the type: the first one's rounding, rounded.
+# Of a value that enters the matrix unit rounded to the type: half an ulp; as the sum of two of the type: the first
+# one's rounding, rounded.
+ONE = {torch.float32: 0.0, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
 SPLIT = {torch.float32: 0.0, torch.float16: 2.0 ** -23, torch.bfloat16: 2.0 ** -17}
 
 
@@ -18,8 +20,8 @@ def attention(q, k, v, g, scale=None, init=None, lengths=None, dtype=torch.float
     The quadratic form: y_i = scale (sum_{j<=i} exp(c_i - c_j) (q_i . k_j) v_j + exp(c_i) S0^T q_i).  What the
     kernel's arithmetic may add is counted against the same sums of magnitudes: K + 1 + (chunks + 1) * 2 fp32 sums
     and products on a way through the states, L more along the tokens; an exponential in base 2 of a difference
-    that fp64 holds costs (|v| + 2) U, one for every chunk that a term passes (their |v| add up); a value that
-    enters as two of the type is off by SPLIT: two of them (v with its decay, then S; or p) on a way."""
+    that fp64 holds costs (|v| + 2) U, one for every chunk that a term passes (their |v| add up).  Of 16-bit
+    types v with its decay enters as two of the type, for S: off by SPLIT; p, or S, as one, for y: off by ONE."""
     b, L, Hq, K = q.shape
     Hk, Hv, V = k.shape[2], v.shape[2], v.shape[3]
     H = max(Hq, Hv)
@@ -38,15 +40,16 @@ def attention(q, k, v, g, scale=None, init=None, lengths=None, dtype=torch.float
     S0 = torch.zeros(b, Hv, K, V, dtype=f64, device=dev) if init is None else init.double()
     S0h = spread(S0, 1, H)
     chunks = -(-L // 32) + 1
-    roundings = (K + L + 4 * chunks + 16) * U + 2 * SPLIT[dtype]
+    roundings = (K + L + 4 * chunks + 16) * U + SPLIT[dtype]
+    of_y = roundings + ONE[dtype]
     diff = c[..., :, None] - c[..., None, :]
     past = torch.ones(L, L, dtype=torch.bool, device=dev).tril()
     W = torch.where(past, torch.exp(torch.where(past, diff, torch.zeros_like(diff))), torch.zeros_like(diff))
     extra = (diff.abs() + 2 * chunks + 2) * U
     y = (W * (qh @ kh.mT)) @ vh + torch.exp(c)[..., None] * (qh @ S0h)
     big = W * (qh.abs() @ kh.abs().mT)
-    e = (big * (roundings + extra)) @ vh.abs()
-    e = e + (torch.exp(c) * (roundings + (c.abs() + 2 * chunks + 2) * U))[..., None] * (qh.abs() @ S0h.abs())
+    e = (big * (of_y + extra)) @ vh.abs()
+    e = e + (torch.exp(c) * (of_y + (c.abs() + 2 * chunks + 2) * U))[..., None] * (qh.abs() @ S0h.abs())
     y, e = (scale * y).transpose(1, 2), (abs(scale) * e).transpose(1, 2)
     y[~live] = 0
     cv = g.cumsum(1).transpose(1, 2)                                  # b Hv L
