@@ -78,10 +78,13 @@ template <typename T> __device__ __forceinline__ Frag<T> rest_frag(const float (
   return round_frag<T>(d);
 }
 
-// The exponent shift that brings magnitude bits `big` of fp32 to [2^14, 2^15); 0 for 0 and for what is no number.
-__device__ __forceinline__ int range_shift(uint32_t big) {
+// fp16: the exponent shift that brings values of which the largest has magnitude bits `big` (fp32) to where they
+// round well: none for a largest one in [2^kLow, 2^15), else to [2^14, 2^15); none for 0 and for what is no number.
+// Below the normal range values are off by 2^-25: of a sum over 64 of them with a largest one of 2^-6 at most 2^-13,
+// less than their own rounding.
+template <int kLow> __device__ __forceinline__ int range_shift(uint32_t big) {
   const int e = (int)(big >> 23);
-  if (e == 0 || e == 255) return 0;
+  if (e == 0 || e == 255 || (e >= 127 + kLow && e < 127 + 15)) return 0;
   const int s = 127 + 14 - e;
   return s > 100 ? 100 : s;
 }
@@ -90,19 +93,19 @@ __device__ __forceinline__ uint32_t bits_max(uint32_t a, float v) {
   const uint32_t m = __builtin_bit_cast(uint32_t, v) & 0x7fffffffu;
   return a > m ? a : m;
 }
-// The largest over the four lane groups, and over all lanes, in each of them.
+// The largest over the four lane groups, in each of them.
 __device__ __forceinline__ uint32_t group_max(uint32_t v) {
   const auto a = __builtin_amdgcn_permlane32_swap(v, v, false, false);
   v = a[0] > a[1] ? a[0] : a[1];
   const auto b = __builtin_amdgcn_permlane16_swap(v, v, false, false);
   return b[0] > b[1] ? b[0] : b[1];
 }
-template <int kCtrl> __device__ __forceinline__ uint32_t lane_max(uint32_t v) {
-  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kCtrl, 0xf, 0xf, true);
-  return v > o ? v : o;
-}
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-  return group_max(lane_max<0x140>(lane_max<0x141>(lane_max<0x4E>(lane_max<0xB1>(v)))));
+// The value of one lane, in scalar registers.
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+  return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
 }
 // Sums over the lanes up to each.
 __device__ __forceinline__ double wave_scan(double v) {
@@ -172,6 +175,13 @@ template <typename T, int kRows, int kWidth, int kPart> struct Stage {
   __device__ __forceinline__ void load(const T* base, uint32_t off, int64_t token_stride, int tokens, int width, int tid) {
     const int in = column(tid) % kPart, row0 = tid / kVecs;
     const auto tile = buffer_of(base);
+    if (tokens >= kRows && width >= kPart) {
+#pragma unroll
+      for (int i = 0; i < kEach; ++i)
+        v[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(
+                                             tile, (int)off, (int)(i * kStep * token_stride * sizeof(T)), 0));
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const uint32_t at = i * kStep + row0 < tokens && in + kPer <= width ? off : kNowhere;
@@ -184,15 +194,16 @@ template <typename T, int kRows, int kWidth, int kPart> struct Stage {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       if (i * kStep + row0 >= tokens) continue;
-      const T* p = reinterpret_cast<const T*>(reinterpret_cast<const char*>(base + i * kStep * token_stride) + off);
       uint64_t half[2] = {0, 0};
 #pragma unroll 1
       for (int j = 0; j < width - in; ++j) {
-        uint64_t e = 0;
-        __builtin_memcpy(&e, p + j, sizeof(T));
-        const uint64_t at = e << (8 * sizeof(T) * (j % (kPer / 2)));
-        half[0] |= j < kPer / 2 ? at : 0;
-        half[1] |= j < kPer / 2 ? 0 : at;
+        const int at = (int)(off + j * (uint32_t)sizeof(T)), row = (int)(i * kStep * token_stride * sizeof(T));
+        uint64_t e;
+        if constexpr (sizeof(T) == 2) e = __builtin_amdgcn_raw_buffer_load_b16(tile, at, row, 0);
+        else e = __builtin_amdgcn_raw_buffer_load_b32(tile, at, row, 0);
+        e <<= 8 * sizeof(T) * (j % (kPer / 2));
+        half[0] |= j < kPer / 2 ? e : 0;
+        half[1] |= j < kPer / 2 ? 0 : e;
       }
       __builtin_memcpy(&v[i], half, 16);
     }
@@ -232,22 +243,21 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
   constexpr bool kHalf = sizeof(T) == 2, kF16 = std::is_same_v<T, _Float16>;
   constexpr int kWH = 4 / kHeads, kSlice = 16 * kTiles * kWH;   // waves of a head, its columns in a workgroup
   constexpr int kSums = kC / 32, kRowsT = kC / 16, kKeyT = kKeys / 16, kKeyS = kKeys / 32;
-  // LDS row lengths.  q is read by rows, 16 bytes of 16 rows at a time: 4 banks from row to row; v by four rows of 32
-  // bytes: 8 banks.  k is read both ways: its rows' chunks of 16 bytes are exchanged (k_at), so that 16 rows at one
-  // chunk, and four rows at four chunks, lie in different banks.
-  constexpr int kPerChunk = 16 / (int)sizeof(T);
-  constexpr int kQ = kKeys + kPerChunk, kV = kSlice * kHeads + 2 * kPerChunk;
-  auto q_at = [](int row, int key) { return row * kQ + key; };
+  // v is read by four rows of 32 bytes: 8 banks from row to row.  Of q and k 16 rows at one chunk of 16 bytes are read
+  // (lanes 0-3, 12-15 and 20-27 of 32 at a time), of k four rows at four chunks, too: chunks are exchanged so that
+  // these lie in different banks.
+  constexpr int kPerChunk = 16 / (int)sizeof(T), kV = kSlice * kHeads + 2 * kPerChunk;
   auto v_at = [](int row, int col) { return row * kV + col; };
   auto k_at = [](int row, int key) {
     constexpr int kChunks = kKeys / kPerChunk;
-    const int f = kChunks >= 16 ? row % 4 * 4 + row / 4 % 4 : row / 2 % 2 * 4 + row / 4 % 4;
+    const int quad = row / 4 % 4, low = ((quad ^ (quad >> 1)) & 1) * 2 + (quad >> 1);   // 0, 2, 3, 1
+    const int f = (kChunks >= 16 ? row % 4 * 4 : row / 2 % 2 * 4) + low;
     // fp32: whole pairs of chunks
     return row * kKeys + ((key / kPerChunk) ^ (kHalf ? f : 2 * f % 16)) * kPerChunk + key % kPerChunk;
   };
   constexpr int kPairs = kRowsT * (kRowsT / 2 + 1) / 2;     // (row tile, 32 tokens) of p that are not 0
   constexpr int kOutSize = kC * kSlice * kHeads;             // of y's tile, which takes the place of q
-  __shared__ __attribute__((aligned(16))) T q_lds[kOut ? (kC * kQ > kOutSize ? kC * kQ : kOutSize) : 8];
+  __shared__ __attribute__((aligned(16))) T q_lds[kOut ? (kC * kKeys > kOutSize ? kC * kKeys : kOutSize) : 8];
   __shared__ __attribute__((aligned(16))) T k_lds[kC * kKeys];
   __shared__ __attribute__((aligned(16))) T v_lds[kC * kV];
   __shared__ __attribute__((aligned(16))) Frag<T> p_lds[kHeads][kOut ? kPairs * 64 : 1];
@@ -342,16 +352,17 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
     // registers that 50 went to memory, where their way back waits for the loads in flight.
     int g = lane_g, m = lane_m;
     asm volatile("" : "+v"(g), "+v"(m));
+    g &= 3, m &= 15;   // their ranges, for the arithmetic of places
     const int lane = g * 16 + m;
     __syncthreads();   // the last chunk is read
-    if constexpr (kOut) q_next.put(q_lds, tid, q_at);
+    if constexpr (kOut) q_next.put(q_lds, tid, k_at);
     k_next.put(k_lds, tid, k_at);
     v_next.put(v_lds, tid, v_at);
     // sums of the decays' logarithms, in base 2; below 2^-65536 is 0 all the same, and an infinite one would leave
     // no differences behind it
     double c = g_next < -65536.0f ? -65536.0 * kLog2e : (double)g_next * kLog2e;
     c = wave_scan(c);
-    const double c_end = __shfl(c, kC - 1);
+    const double c_end = lane_value(c, kC - 1);
     if (hw == 0 && lane < kC) {
       c_lds[lane] = c;
       w_lds[lane] = __builtin_amdgcn_exp2f((float)(c_end - c));
@@ -372,7 +383,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         v4f acc[kRowsT] = {};
 #pragma unroll
         for (int s = 0; s < kKeyS; ++s) {
-          const Frag<T> qf = row_frag(q_lds + q_at(i, 32 * s + 8 * g));
+          const Frag<T> qf = row_frag(q_lds + k_at(i, 32 * s + 8 * g));
 #pragma unroll
           for (int jt = 0; jt < kRowsT; ++jt)
             if (jt < most) acc[jt] = mma(row_frag(k_lds + k_at(jt * 16 + m, 32 * s + 8 * g)), qf, acc[jt]);
@@ -409,11 +420,15 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
 #pragma unroll
           for (int r = 0; r < 4; ++r) big = __builtin_fmaxf(big, __builtin_fabsf(acc[jt][r]));
         }
-        float up = 1.0f;
         if constexpr (kF16) {
-          const int s = range_shift(group_max(__builtin_bit_cast(uint32_t, big)));
-          up = power(s);
-          if (g == 0) row_scale[i] = up;
+          const int sh = range_shift<-6>(group_max(__builtin_bit_cast(uint32_t, big)));
+          if (g == 0) row_scale[i] = power(sh);
+          if (__any(sh != 0)) {
+#pragma unroll
+            for (int jt = 0; jt < kRowsT; ++jt)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[jt][r] *= power(sh);
+          }
         }
         const int pair0 = it / 2 * (it / 2 + 1) + it % 2 * (it / 2 + 1);
 #pragma unroll
@@ -421,30 +436,29 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           if (2 * s > it) continue;
           float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = kF16 ? acc[2 * s + e / 4][e % 4] * up : acc[2 * s + e / 4][e % 4];
+          for (int e = 0; e < 8; ++e) f[e] = acc[2 * s + e / 4][e % 4];
           p_lds[sub][(pair0 + s) * 64 + lane] = round_frag<T>(f);
         }
       }
     }
 
     v4f acc[kOut ? kRowsT : 1][kTiles] = {};
-    float s_down[kTiles];
+    int s_shift[kTiles];        // of the lane's column of the state
+    bool any_shift = false;
     if constexpr (kOut) {
       // S^T q, the state rounded to the type
       __builtin_amdgcn_sched_barrier(0);   // phases stay apart: their operands do not fit the registers together
-      float s_up[kTiles];
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
-        s_up[n] = s_down[n] = 1.0f;
+        s_shift[n] = 0;
         if constexpr (kF16) {
           float most = 0.0f;
 #pragma unroll
           for (int t = 0; t < kKeyT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) most = __builtin_fmaxf(most, __builtin_fabsf(S[t][n][r]));
-          const int sh = range_shift(wave_max(__builtin_bit_cast(uint32_t, most)));
-          s_up[n] = power(sh);
-          s_down[n] = power(-sh);
+          s_shift[n] = range_shift<-6>(group_max(__builtin_bit_cast(uint32_t, most)));
+          any_shift |= __any(s_shift[n] != 0) != 0;
         }
       }
 #pragma unroll
@@ -454,16 +468,16 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         for (int n = 0; n < kTiles; ++n) {
           float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = kF16 ? S[2 * s + e / 4][n][e % 4] * s_up[n] : S[2 * s + e / 4][n][e % 4];
+          for (int e = 0; e < 8; ++e) f[e] = kF16 ? S[2 * s + e / 4][n][e % 4] * power(s_shift[n]) : S[2 * s + e / 4][n][e % 4];
           sf[n] = round_frag<T>(f);
         }
 #pragma unroll
         for (int it = 0; it < kRowsT; ++it) {
-          const Frag<T> qf = row_frag(q_lds + q_at(it * 16 + m, 32 * s + 8 * g));
+          const Frag<T> qf = row_frag(q_lds + k_at(it * 16 + m, 32 * s + 8 * g));
 #pragma unroll
           for (int n = 0; n < kTiles; ++n) acc[it][n] = mma(sf[n], qf, acc[it][n]);
         }
-        if (s % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+        if (kF16 || s % 2 == 1) __builtin_amdgcn_sched_barrier(0);
       }
       __syncthreads();   // p is there
     }
@@ -472,24 +486,30 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
     Frag<T> vf[kSums][kTiles];
     uint32_t most_v[kTiles];
     int first[kTiles];   // the first token of the column whose value is no number
-    bool any_bad = false;
+    constexpr uint32_t kNoNumber = kF16 ? 0x7c00u : kHalf ? 0x7f80u : 0x7f800000u;
+    auto largest_v = [&](int n) {
+      uint32_t big = 0;
+#pragma unroll
+      for (int s = 0; s < kSums; ++s) big = largest(vf[s][n], big);
+      return !kHalf ? big : (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
+    };
+    bool odd = false;
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      uint32_t big = 0;
       first[n] = kC;
 #pragma unroll
-      for (int s = 0; s < kSums; ++s) {
+      for (int s = 0; s < kSums; ++s)
         vf[s][n] = column_frag(v_lds + 32 * s * kV + sub * kSlice + my0 + 16 * n, lane,
                                [&](int row, int c) { return v_at(row, 4 * c); });
-        big = largest(vf[s][n], big);
-      }
-      if constexpr (kHalf) big = (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
-      const bool odd = big >= (kF16 ? 0x7c00u : kHalf ? 0x7f80u : 0x7f800000u);
-      if (__any(odd)) {
-        any_bad = true;
-        big = 0;
+      most_v[n] = largest_v(n);
+      odd |= most_v[n] >= kNoNumber;
+    }
+    const bool any_bad = __any(odd) != 0;
+    if (any_bad) {
 #pragma unroll
-        for (int s = 0; s < kSums; ++s) {
+      for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+        for (int s = 0; s < kSums; ++s)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             if (!(__builtin_fabsf((float)vf[s][n].v[e]) < __builtin_inff())) {
@@ -497,48 +517,66 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
               first[n] = j < first[n] ? j : first[n];
               vf[s][n].v[e] = (T)0.0f;
             }
-          big = largest(vf[s][n], big);
-        }
-        if constexpr (kHalf) big = (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
+        most_v[n] = largest_v(n);
 #pragma unroll
         for (int d = 16; d < 64; d *= 2) {
           const int o = __shfl_xor(first[n], d);
           first[n] = o < first[n] ? o : first[n];
         }
       }
-      most_v[n] = big;
     }
 
     if constexpr (kOut) {
 #pragma unroll
       for (int it = 0; it < kRowsT; ++it) {
         const int i = it * 16 + m;
-        const float e = e_lds[i], in = kF16 ? row_scale[i] : 1.0f;
-        const float out = kF16 ? 1.0f / in : 1.0f;   // of a power of two: exact
-#pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-          const float by = kF16 ? e * s_down[n] * in : e;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[it][n][r] *= by;
-        }
-        const int pair0 = it / 2 * (it / 2 + 1) + it % 2 * (it / 2 + 1);
-#pragma unroll
-        for (int s = 0; s < kSums; ++s)
-          if (2 * s <= it) {
-            const Frag<T> pf = p_lds[sub][(pair0 + s) * 64 + lane];
-#pragma unroll
-            for (int n = 0; n < kTiles; ++n) acc[it][n] = mma(vf[s][n], pf, acc[it][n]);
-          }
+        float e = e_lds[i];
+        if constexpr (kF16) e *= row_scale[i];   // as p's rows are
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[it][n][r] *= out;
-          if (any_bad) {
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-              if (i >= __shfl(first[n], 4 * g + r)) acc[it][n][r] = __builtin_nanf("");
-          }
+          for (int r = 0; r < 4; ++r) acc[it][n][r] *= e;
         }
+      }
+      if (any_shift) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const float by = power(-__shfl(s_shift[n], 4 * g + r));
+#pragma unroll
+            for (int it = 0; it < kRowsT; ++it) acc[it][n][r] *= by;
+          }
+      }
+#pragma unroll
+      for (int s = 0; s < kSums; ++s)
+#pragma unroll
+        for (int it = 2 * s; it < kRowsT; ++it) {
+          const int pair0 = it / 2 * (it / 2 + 1) + it % 2 * (it / 2 + 1);
+          const Frag<T> pf = p_lds[sub][(pair0 + s) * 64 + lane];
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) acc[it][n] = mma(vf[s][n], pf, acc[it][n]);
+        }
+      if constexpr (kF16) {
+#pragma unroll
+        for (int it = 0; it < kRowsT; ++it) {
+          const float out = __builtin_amdgcn_rcpf(row_scale[it * 16 + m]);   // of a power of two: exact
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[it][n][r] *= out;
+        }
+      }
+      if (any_bad) {
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int from = __shfl(first[n], 4 * g + r);
+#pragma unroll
+            for (int it = 0; it < kRowsT; ++it)
+              if (it * 16 + m >= from) acc[it][n][r] = __builtin_nanf("");
+          }
       }
       __builtin_amdgcn_sched_barrier(0);
       // y leaves through the place of q, which all waves have read: the wave's rows in whole vectors of 16 bytes.
@@ -590,30 +628,32 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           for (int row = row0; row < rows; row += 64 / kChunks) {
             const T* from = reinterpret_cast<const T*>(out_lds + (row * kChunks + (x ^ (row / kPeriod % kChunks))) * 16);
 #pragma unroll 1
-            for (int c = 0; c < mine; ++c) y[(int64_t)row * y_row + x * kPer + c] = from[c];
+            for (int c = 0; c < mine; ++c) {
+              const int at = (row * y_row + x * kPer + c) * (int)sizeof(T);
+              if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, from[c]), tile, at, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, from[c]), tile, at, 0, 0);
+            }
           }
       }
     }
-    if (chunk + 1 < last) request(chunk + 1);
-
     __builtin_amdgcn_sched_barrier(0);
     // The state behind the chunk: v times exp(c_end - c_j), as two values of the type
     const float decay = __builtin_amdgcn_exp2f((float)c_end);
-    float up[kTiles], down[kTiles];
+    int v_shift[kTiles];
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      up[n] = down[n] = 1.0f;
+      v_shift[n] = 0;
       if constexpr (kF16) {
         // as fp32's bits; the decays only make the values smaller
         const float most = (float)__builtin_bit_cast(_Float16, (uint16_t)group_max(most_v[n]));
-        const int sh = range_shift(__builtin_bit_cast(uint32_t, most));
-        up[n] = power(sh);
-        down[n] = power(-sh);
+        v_shift[n] = range_shift<-2>(__builtin_bit_cast(uint32_t, most));
       }
+      // a column with a value that is no number is NaN from here on
+      const float by = first[n] < kC ? __builtin_nanf("") : kF16 ? decay * power(v_shift[n]) : decay;
 #pragma unroll
       for (int t = 0; t < kKeyT; ++t)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[t][n][r] *= kF16 ? decay * up[n] : decay;
+        for (int r = 0; r < 4; ++r) S[t][n][r] *= by;
     }
 #pragma unroll
     for (int s = 0; s < kSums; ++s) {
@@ -625,37 +665,32 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
       for (int n = 0; n < kTiles; ++n) {
         float f[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * (kF16 ? w[e] * up[n] : w[e]);
+        for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * (kF16 ? w[e] * power(v_shift[n]) : w[e]);
         whi[n] = round_frag<T>(f);
         if constexpr (kHalf) wlo[n] = rest_frag(f, whi[n]);
       }
 #pragma unroll
       for (int t = 0; t < kKeyT; ++t) {
-        const Frag<T> kf = column_frag(k_lds, lane, [&](int row, int c) { return k_at(32 * s + row, key_of(t, c)); });
+        const Frag<T> kf = column_frag(k_lds + 32 * s * kKeys, lane, [&](int row, int c) { return k_at(row, key_of(t, c)); });
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) {
-          S[t][n] = mma(kf, whi[n], S[t][n]);
-          if constexpr (kHalf) S[t][n] = mma(kf, wlo[n], S[t][n]);
-        }
+        for (int n = 0; n < kTiles; ++n) S[t][n] = mma(kf, whi[n], S[t][n]);
+        if constexpr (kHalf)
+#pragma unroll
+          for (int n = 0; n < kTiles; ++n) S[t][n] = mma(kf, wlo[n], S[t][n]);
       }
-      __builtin_amdgcn_sched_barrier(0);
+      // the next chunk's loads, where registers for them are free
+      if (s == 0) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (chunk + 1 < last) request(chunk + 1);
+      }
     }
-    if constexpr (kF16) {
+    if constexpr (kF16) {   // without a branch, which would have S in the registers twice
 #pragma unroll
       for (int n = 0; n < kTiles; ++n)
 #pragma unroll
         for (int t = 0; t < kKeyT; ++t)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[t][n][r] *= down[n];
-    }
-    if (any_bad) {
-#pragma unroll
-      for (int n = 0; n < kTiles; ++n)
-        if (first[n] < kC)
-#pragma unroll
-          for (int t = 0; t < kKeyT; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) S[t][n][r] = __builtin_nanf("");
+          for (int r = 0; r < 4; ++r) S[t][n][r] *= power(-v_shift[n]);
     }
     total += c_end;
   }
