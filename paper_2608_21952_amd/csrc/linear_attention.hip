@@ -144,6 +144,9 @@ template <typename T, typename At> __device__ __forceinline__ Frag<T> column_fra
   return f;
 }
 
+// A condition whose code is to lie out of the way.
+__device__ __forceinline__ bool rarely(bool v) { return __builtin_expect(v, 0); }
+
 struct Args {
   LinearAttention a;
   int slices, spans, chunks, span_chunks;   // column slices of a head; spans of the tokens and their chunks
@@ -175,7 +178,7 @@ template <typename T, int kRows, int kWidth, int kPart> struct Stage {
   __device__ __forceinline__ void load(const T* base, uint32_t off, int64_t token_stride, int tokens, int width, int tid) {
     const int in = column(tid) % kPart, row0 = tid / kVecs;
     const auto tile = buffer_of(base);
-    if (tokens >= kRows && width >= kPart) {
+    if (!rarely(tokens < kRows || width < kPart)) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i)
         v[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(
@@ -188,7 +191,7 @@ template <typename T, int kRows, int kWidth, int kPart> struct Stage {
       const auto d = __builtin_amdgcn_raw_buffer_load_b128(tile, (int)at, (int)(i * kStep * token_stride * sizeof(T)), 0);
       v[i] = __builtin_bit_cast(uint4, d);
     }
-    if (width % kPer == 0) return;
+    if (!rarely(width % kPer != 0)) return;
     // the row's last vector, value by value
     if (in >= width || in + kPer <= width) return;
 #pragma unroll
@@ -423,7 +426,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         if constexpr (kF16) {
           const int sh = range_shift<-6>(group_max(__builtin_bit_cast(uint32_t, big)));
           if (g == 0) row_scale[i] = power(sh);
-          if (__any(sh != 0)) {
+          if (rarely(__any(sh != 0))) {
 #pragma unroll
             for (int jt = 0; jt < kRowsT; ++jt)
 #pragma unroll
@@ -505,7 +508,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
       odd |= most_v[n] >= kNoNumber;
     }
     const bool any_bad = __any(odd) != 0;
-    if (any_bad) {
+    if (rarely(any_bad)) {
 #pragma unroll
       for (int n = 0; n < kTiles; ++n) {
 #pragma unroll
@@ -538,7 +541,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           for (int r = 0; r < 4; ++r) acc[it][n][r] *= e;
         }
       }
-      if (any_shift) {
+      if (rarely(any_shift)) {
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -567,7 +570,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
             for (int r = 0; r < 4; ++r) acc[it][n][r] *= out;
         }
       }
-      if (any_bad) {
+      if (rarely(any_bad)) {
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
@@ -584,7 +587,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
       constexpr int kChunks = kTiles * (int)sizeof(T), kPeriod = 16 / kChunks, kPer = 16 / (int)sizeof(T);
       char* out_lds = reinterpret_cast<char*>(q_lds) + wave * kC * kChunks * 16;
       const int64_t left = end - t0;
-      if (left < kC) {   // tokens behind the sequence's end: 0
+      if (rarely(left < kC)) {   // tokens behind the sequence's end: 0
 #pragma unroll
         for (int it = 0; it < kRowsT; ++it)
 #pragma unroll
@@ -622,7 +625,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         const uint32_t at = row < rows && mine >= kPer ? y_off + step : kNowhere;
         __builtin_amdgcn_raw_buffer_store_b128(v, tile, (int)at, 0, 0);
       }
-      if (cols - my0 < 16 * kTiles && cols % kPer) {   // the rows' last vectors, value by value
+      if (rarely(cols - my0 < 16 * kTiles && cols % kPer != 0)) {   // the rows' last vectors, value by value
         if (mine > 0 && mine < kPer)
 #pragma unroll 1
           for (int row = row0; row < rows; row += 64 / kChunks) {
