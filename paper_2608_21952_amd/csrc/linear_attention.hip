@@ -175,20 +175,21 @@ template <typename T, int kRows, int kWidth, int kPart> struct Stage {
     const int c = column(tid);
     return (uint32_t)((tid / kVecs * token_stride + (kPart < kWidth ? c / kPart * part : 0) + c % kPart) * sizeof(T));
   }
-  __device__ __forceinline__ void load(const T* base, uint32_t off, int64_t token_stride, int tokens, int width, int tid) {
+  // step: bytes from a load's rows to the next one's
+  __device__ __forceinline__ void load(const char* base, uint32_t off, uint32_t step, int tokens, int width, int tid) {
     const int in = column(tid) % kPart, row0 = tid / kVecs;
     const auto tile = buffer_of(base);
     if (!rarely(tokens < kRows || width < kPart)) {
 #pragma unroll
       for (int i = 0; i < kEach; ++i)
         v[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(
-                                             tile, (int)off, (int)(i * kStep * token_stride * sizeof(T)), 0));
+                                             tile, (int)off, (int)(i * step), 0));
       return;
     }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const uint32_t at = i * kStep + row0 < tokens && in + kPer <= width ? off : kNowhere;
-      const auto d = __builtin_amdgcn_raw_buffer_load_b128(tile, (int)at, (int)(i * kStep * token_stride * sizeof(T)), 0);
+      const auto d = __builtin_amdgcn_raw_buffer_load_b128(tile, (int)at, (int)(i * step), 0);
       v[i] = __builtin_bit_cast(uint4, d);
     }
     if (!rarely(width % kPer != 0)) return;
@@ -200,7 +201,7 @@ template <typename T, int kRows, int kWidth, int kPart> struct Stage {
       uint64_t half[2] = {0, 0};
 #pragma unroll 1
       for (int j = 0; j < width - in; ++j) {
-        const int at = (int)(off + j * (uint32_t)sizeof(T)), row = (int)(i * kStep * token_stride * sizeof(T));
+        const int at = (int)(off + j * (uint32_t)sizeof(T)), row = (int)(i * step);
         uint64_t e;
         if constexpr (sizeof(T) == 2) e = __builtin_amdgcn_raw_buffer_load_b16(tile, at, row, 0);
         else e = __builtin_amdgcn_raw_buffer_load_b32(tile, at, row, 0);
@@ -335,21 +336,45 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
   typedef Stage<T, kC, kSlice * kHeads, kSlice> ValueStage;
   KeyStage q_next, k_next;
   ValueStage v_next;
+  // Where the next chunk to be loaded and the next one to be stored begin, and steps in bytes: running values, as the
+  // products with the strides and their way from the arguments took as long as a chunk's matrix products.
+  const int64_t t_first = (int64_t)chunk0 * kC;
+  const char *q_from = reinterpret_cast<const char*>(qp + t_first * a.qs.token),
+             *k_from = reinterpret_cast<const char*>(kp + t_first * a.ks.token),
+             *v_from = reinterpret_cast<const char*>(vp + t_first * a.vs.token);
+  const uint32_t q_row = (uint32_t)(a.qs.token * sizeof(T)), k_row = (uint32_t)(a.ks.token * sizeof(T)),
+                 v_row = (uint32_t)(a.vs.token * sizeof(T)), y_row = (uint32_t)(a.heads * a.values * sizeof(T));
+  char* y_to = reinterpret_cast<char*>(static_cast<T*>(a.y) + ((b * a.seqlen + t_first) * a.heads + h) * a.values + col0 + my0);
+  const float* g_from = !a.log_decay ? nullptr
+                        : a.token_decay ? a.log_decay + b * a.g_batch + t_first * a.g_token + hv : a.log_decay + hv;
+  const int64_t g_row = a.log_decay && a.token_decay ? a.g_token : 0;
   const uint32_t q_off = KeyStage::offset(a.qs.token, 0, tid), k_off = KeyStage::offset(a.ks.token, 0, tid);
   const uint32_t v_off = ValueStage::offset(a.vs.token, a.vs.head, tid);
   float g_next = 0.0f;
-  auto request = [&](int chunk) {
+  // The chunk behind the one requested last, in three pieces.
+  auto request = [&](int chunk, int piece) {
     const int64_t t0 = (int64_t)chunk * kC;
     const int tokens = (int)(end - t0 < kC ? end - t0 : kC);
-    if constexpr (kOut) q_next.load(qp + t0 * a.qs.token, q_off, a.qs.token, tokens, keys, tid);
-    k_next.load(kp + t0 * a.ks.token, k_off, a.ks.token, tokens, keys, tid);
-    v_next.load(vp + t0 * a.vs.token, v_off, a.vs.token, tokens, cols, tid);
-    g_next = 0.0f;
-    if (a.log_decay && lane < tokens)
-      g_next = a.token_decay ? a.log_decay[b * a.g_batch + (t0 + lane) * a.g_token + hv] : a.log_decay[hv];
+    if (piece == 0) {
+      g_next = 0.0f;
+      if (g_from && lane < tokens) g_next = g_from[lane * g_row];
+      if (g_from) g_from += kC * g_row;
+      k_next.load(k_from, k_off, KeyStage::kStep * k_row, tokens, keys, tid);
+      k_from += (int64_t)kC * k_row;
+    } else if (piece == 1) {
+      v_next.load(v_from, v_off, ValueStage::kStep * v_row, tokens, cols, tid);
+      v_from += (int64_t)kC * v_row;
+    } else if constexpr (kOut) {
+      q_next.load(q_from, q_off, KeyStage::kStep * q_row, tokens, keys, tid);
+      q_from += (int64_t)kC * q_row;
+    }
   };
 
-  if (chunk0 < last) request(chunk0);
+  if (chunk0 < last) {
+    request(chunk0, 0);
+    request(chunk0, 1);
+    request(chunk0, 2);
+  }
   for (int chunk = chunk0; chunk < last; ++chunk) {
     // The lane's places are formed anew for every chunk: kept over all of them, places and constants took up so many
     // registers that 50 went to memory, where their way back waits for the loads in flight.
@@ -374,6 +399,50 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
     __syncthreads();
 
     const int64_t t0 = (int64_t)chunk * kC;
+    // v, 0 where its values are no numbers
+    Frag<T> vf[kSums][kTiles];
+    uint32_t most_v[kTiles];
+    int first[kTiles];   // the first token of the column whose value is no number
+    constexpr uint32_t kNoNumber = kF16 ? 0x7c00u : kHalf ? 0x7f80u : 0x7f800000u;
+    auto largest_v = [&](int n) {
+      uint32_t big = 0;
+#pragma unroll
+      for (int s = 0; s < kSums; ++s) big = largest(vf[s][n], big);
+      return !kHalf ? big : (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
+    };
+    bool odd = false;
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+      first[n] = kC;
+#pragma unroll
+      for (int s = 0; s < kSums; ++s)
+        vf[s][n] = column_frag(v_lds + 32 * s * kV + sub * kSlice + my0 + 16 * n, lane,
+                               [&](int row, int c) { return v_at(row, 4 * c); });
+      most_v[n] = largest_v(n);
+      odd |= most_v[n] >= kNoNumber;
+    }
+    const bool any_bad = __any(odd) != 0;
+    if (rarely(any_bad)) {
+#pragma unroll
+      for (int n = 0; n < kTiles; ++n) {
+#pragma unroll
+        for (int s = 0; s < kSums; ++s)
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (!(__builtin_fabsf((float)vf[s][n].v[e]) < __builtin_inff())) {
+              const int j = 32 * s + 16 * (e / 4) + 4 * g + e % 4;
+              first[n] = j < first[n] ? j : first[n];
+              vf[s][n].v[e] = (T)0.0f;
+            }
+        most_v[n] = largest_v(n);
+#pragma unroll
+        for (int d = 16; d < 64; d *= 2) {
+          const int o = __shfl_xor(first[n], d);
+          first[n] = o < first[n] ? o : first[n];
+        }
+      }
+    }
+
     if constexpr (kOut) {
       // p^T: rows j, column i = m of row tile it; the waves of a head take one from each end of them in turn
 #pragma unroll
@@ -381,16 +450,6 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         const int it = u % 2 == 0 ? u * kWH + hw : (u + 1) * kWH - 1 - hw;
         if (it >= kRowsT) continue;
         const int i = it * 16 + m;
-        constexpr int kAll = kRowsT;
-        const int most = (u + 1) * kWH < kAll ? (u + 1) * kWH : kAll;   // tiles that any wave has in this turn
-        v4f acc[kRowsT] = {};
-#pragma unroll
-        for (int s = 0; s < kKeyS; ++s) {
-          const Frag<T> qf = row_frag(q_lds + k_at(i, 32 * s + 8 * g));
-#pragma unroll
-          for (int jt = 0; jt < kRowsT; ++jt)
-            if (jt < most) acc[jt] = mma(row_frag(k_lds + k_at(jt * 16 + m, 32 * s + 8 * g)), qf, acc[jt]);
-        }
         // exp(c_i - c_j) for tokens j of earlier row tiles is exp(c_i - c_x) exp(c_x - c_j), x the last of them: both
         // at most 1, the second one for all rows
         const double ci = c_lds[i], cx = c_lds[it > 0 ? it * 16 - 1 : 0];
@@ -402,6 +461,16 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         float wd[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) wd[r] = a.scale * __builtin_amdgcn_exp2f((float)(ci - cj[r]));
+        constexpr int kAll = kRowsT;
+        const int most = (u + 1) * kWH < kAll ? (u + 1) * kWH : kAll;   // tiles that any wave has in this turn
+        v4f acc[kRowsT] = {};
+#pragma unroll
+        for (int s = 0; s < kKeyS; ++s) {
+          const Frag<T> qf = row_frag(q_lds + k_at(i, 32 * s + 8 * g));
+#pragma unroll
+          for (int jt = 0; jt < kRowsT; ++jt)
+            if (jt < most) acc[jt] = mma(row_frag(k_lds + k_at(jt * 16 + m, 32 * s + 8 * g)), qf, acc[jt]);
+        }
         __builtin_amdgcn_wave_barrier();
         float big = 0.0f;
 #pragma unroll
@@ -464,8 +533,15 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           any_shift |= __any(s_shift[n] != 0) != 0;
         }
       }
+      Frag<T> qf[2][kRowsT];   // read a step ahead
+      auto read_q = [&](int s) {
+#pragma unroll
+        for (int it = 0; it < kRowsT; ++it) qf[s % 2][it] = row_frag(q_lds + k_at(it * 16 + m, 32 * s + 8 * g));
+      };
+      read_q(0);
 #pragma unroll
       for (int s = 0; s < kKeyS; ++s) {
+        if (s + 1 < kKeyS) read_q(s + 1);
         Frag<T> sf[kTiles];
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
@@ -475,58 +551,12 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           sf[n] = round_frag<T>(f);
         }
 #pragma unroll
-        for (int it = 0; it < kRowsT; ++it) {
-          const Frag<T> qf = row_frag(q_lds + k_at(it * 16 + m, 32 * s + 8 * g));
+        for (int it = 0; it < kRowsT; ++it)
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) acc[it][n] = mma(sf[n], qf, acc[it][n]);
-        }
-        if (kF16 || s % 2 == 1) __builtin_amdgcn_sched_barrier(0);
+          for (int n = 0; n < kTiles; ++n) acc[it][n] = mma(sf[n], qf[s % 2][it], acc[it][n]);
+        __builtin_amdgcn_sched_barrier(0);
       }
       __syncthreads();   // p is there
-    }
-
-    // v, 0 where its values are no numbers
-    Frag<T> vf[kSums][kTiles];
-    uint32_t most_v[kTiles];
-    int first[kTiles];   // the first token of the column whose value is no number
-    constexpr uint32_t kNoNumber = kF16 ? 0x7c00u : kHalf ? 0x7f80u : 0x7f800000u;
-    auto largest_v = [&](int n) {
-      uint32_t big = 0;
-#pragma unroll
-      for (int s = 0; s < kSums; ++s) big = largest(vf[s][n], big);
-      return !kHalf ? big : (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
-    };
-    bool odd = false;
-#pragma unroll
-    for (int n = 0; n < kTiles; ++n) {
-      first[n] = kC;
-#pragma unroll
-      for (int s = 0; s < kSums; ++s)
-        vf[s][n] = column_frag(v_lds + 32 * s * kV + sub * kSlice + my0 + 16 * n, lane,
-                               [&](int row, int c) { return v_at(row, 4 * c); });
-      most_v[n] = largest_v(n);
-      odd |= most_v[n] >= kNoNumber;
-    }
-    const bool any_bad = __any(odd) != 0;
-    if (rarely(any_bad)) {
-#pragma unroll
-      for (int n = 0; n < kTiles; ++n) {
-#pragma unroll
-        for (int s = 0; s < kSums; ++s)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (!(__builtin_fabsf((float)vf[s][n].v[e]) < __builtin_inff())) {
-              const int j = 32 * s + 16 * (e / 4) + 4 * g + e % 4;
-              first[n] = j < first[n] ? j : first[n];
-              vf[s][n].v[e] = (T)0.0f;
-            }
-        most_v[n] = largest_v(n);
-#pragma unroll
-        for (int d = 16; d < 64; d *= 2) {
-          const int o = __shfl_xor(first[n], d);
-          first[n] = o < first[n] ? o : first[n];
-        }
-      }
     }
 
     if constexpr (kOut) {
@@ -608,11 +638,9 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         }
       __builtin_amdgcn_wave_barrier();
       const int rows = (int)(a.seqlen - t0 < kC ? a.seqlen - t0 : kC);
-      T* y = static_cast<T*>(a.y) + ((b * a.seqlen + t0) * a.heads + h) * a.values + col0 + my0;
-      const auto tile = buffer_of(y);
+      const auto tile = buffer_of(y_to);
       const int x = lane % kChunks, row0 = lane / kChunks, mine = cols - my0 - x * kPer;   // columns from mine on
-      const int y_row = (int)(a.heads * a.values);
-      const uint32_t y_off = (uint32_t)(row0 * y_row + x * kPer) * (uint32_t)sizeof(T);
+      const uint32_t y_off = (uint32_t)row0 * y_row + (uint32_t)(x * kPer * (int)sizeof(T));
 #pragma unroll
       for (int u = 0; u < kC * kChunks / 64; ++u) {
         const int row = u * (64 / kChunks) + row0;
@@ -621,10 +649,11 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         // The whole offset in the vector register: with a part of it in a scalar one the compiler leaves out the wait
         // state between a store of 16 bytes and the next write to its data registers, and the hardware stored the
         // first four bytes of some lanes from what was written there next.
-        const uint32_t step = (uint32_t)(u * (64 / kChunks) * y_row) * (uint32_t)sizeof(T);
+        const uint32_t step = (uint32_t)(u * (64 / kChunks)) * y_row;
         const uint32_t at = row < rows && mine >= kPer ? y_off + step : kNowhere;
         __builtin_amdgcn_raw_buffer_store_b128(v, tile, (int)at, 0, 0);
       }
+      y_to += (int64_t)kC * y_row;
       if (rarely(cols - my0 < 16 * kTiles && cols % kPer != 0)) {   // the rows' last vectors, value by value
         if (mine > 0 && mine < kPer)
 #pragma unroll 1
@@ -632,7 +661,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
             const T* from = reinterpret_cast<const T*>(out_lds + (row * kChunks + (x ^ (row / kPeriod % kChunks))) * 16);
 #pragma unroll 1
             for (int c = 0; c < mine; ++c) {
-              const int at = (row * y_row + x * kPer + c) * (int)sizeof(T);
+              const int at = (int)((uint32_t)row * y_row) + (x * kPer + c) * (int)sizeof(T);
               if constexpr (sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, from[c]), tile, at, 0, 0);
               else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, from[c]), tile, at, 0, 0);
             }
@@ -658,34 +687,52 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[t][n][r] *= by;
     }
+    // k's columns are read four key tiles ahead: each read at its use, the products waited for it 16 times (4000 to
+    // 5700 cycles for 1024 of products).
+    constexpr int kAhead = kKeyT < 4 ? kKeyT : 4, kParts = kSums * kKeyT / kAhead;
+    Frag<T> kf[2][kAhead];
+    auto read_k = [&](int part) {
 #pragma unroll
-    for (int s = 0; s < kSums; ++s) {
-      Frag<T> whi[kTiles], wlo[kTiles];
-      const float4 wa = *reinterpret_cast<const float4*>(w_lds + 32 * s + 4 * g);
-      const float4 wb = *reinterpret_cast<const float4*>(w_lds + 32 * s + 16 + 4 * g);
-      const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
+      for (int u = 0; u < kAhead; ++u) {
+        const int s = part * kAhead / kKeyT, t = part * kAhead % kKeyT + u;
+        kf[part % 2][u] = column_frag(k_lds + 32 * s * kKeys, lane, [&](int row, int c) { return k_at(row, key_of(t, c)); });
+      }
+    };
+    read_k(0);
+    Frag<T> whi[kTiles], wlo[kTiles];
 #pragma unroll
-      for (int n = 0; n < kTiles; ++n) {
-        float f[8];
+    for (int part = 0; part < kParts; ++part) {
+      const int s = part * kAhead / kKeyT, t0 = part * kAhead % kKeyT;
+      if (part + 1 < kParts) read_k(part + 1);
+      if (t0 == 0) {
+        const float4 wa = *reinterpret_cast<const float4*>(w_lds + 32 * s + 4 * g);
+        const float4 wb = *reinterpret_cast<const float4*>(w_lds + 32 * s + 16 + 4 * g);
+        const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * (kF16 ? w[e] * power(v_shift[n]) : w[e]);
-        whi[n] = round_frag<T>(f);
-        if constexpr (kHalf) wlo[n] = rest_frag(f, whi[n]);
+        for (int n = 0; n < kTiles; ++n) {
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * (kF16 ? w[e] * power(v_shift[n]) : w[e]);
+          whi[n] = round_frag<T>(f);
+          if constexpr (kHalf) wlo[n] = rest_frag(f, whi[n]);
+        }
       }
 #pragma unroll
-      for (int t = 0; t < kKeyT; ++t) {
-        const Frag<T> kf = column_frag(k_lds + 32 * s * kKeys, lane, [&](int row, int c) { return k_at(row, key_of(t, c)); });
+      for (int u = 0; u < kAhead; ++u) {
+        const Frag<T>& k = kf[part % 2][u];
+        const int t = t0 + u;
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) S[t][n] = mma(kf, whi[n], S[t][n]);
+        for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, whi[n], S[t][n]);
         if constexpr (kHalf)
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) S[t][n] = mma(kf, wlo[n], S[t][n]);
+          for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, wlo[n], S[t][n]);
       }
-      // the next chunk's loads, where registers for them are free
-      if (s == 0) {
-        __builtin_amdgcn_sched_barrier(0);
-        if (chunk + 1 < last) request(chunk + 1);
-      }
+      __builtin_amdgcn_sched_barrier(0);
+      // the next chunk's loads, between the products: all at once they hold the wave up while they are issued (12
+      // of 16 bytes per lane, 1700 to 3000 cycles)
+      if (chunk + 1 < last)
+#pragma unroll
+        for (int piece = part * 3 / kParts; piece < (part + 1) * 3 / kParts; ++piece) request(chunk + 1, piece);
     }
     if constexpr (kF16) {   // without a branch, which would have S in the registers twice
 #pragma unroll
