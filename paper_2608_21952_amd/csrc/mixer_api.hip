@@ -170,7 +170,9 @@ ssdi8_status ssdi8_norm_quantize(int64_t rows, int64_t channels, int64_t groups,
 
 ssdi8_status ssdi8_quantize_mx(int64_t rows, int64_t k, const void* x, int dtype, int64_t x_row_stride,
                                int format, void* codes, void* scales, void* stream) {
-  if (bad_size(rows, 0) || bad_size(k, 1) || (double)rows * (k + 32) > kMaxCount) return SSDI8_ERR_SHAPE;
+  if (bad_size(rows, 0) || bad_size(k, 1) || (double)rows * (k + 32) > kMaxCount ||
+      (double)rows * (k + 32) / 8192 + 1 > kMaxGrid)
+    return SSDI8_ERR_SHAPE;
   if (!is_float(dtype) || (format != SSDI8_FMT_MXFP8 && format != SSDI8_FMT_MXFP4)) return SSDI8_ERR_ARG;
   if (bad_stride(x_row_stride)) return SSDI8_ERR_SHAPE;
   if (rows == 0) return SSDI8_OK;

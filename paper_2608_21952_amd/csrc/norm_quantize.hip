@@ -27,12 +27,15 @@ struct Args {
   float eps, inv;
 };
 
-// The codes of a vector of y, n values of it, at channel `at` of a row: int8 with the row's step.
-__device__ __forceinline__ void put_int8(const Args& a, int64_t row, int at, int n, const float (&v)[kVec], float inv) {
-  uint8_t c[kVec];
+__device__ __forceinline__ void int8_codes(const float (&v)[kVec], float inv, uint8_t (&c)[kVec]) {
 #pragma unroll
   for (int e = 0; e < kVec; ++e)
     c[e] = (uint8_t)(int8_t)(int)__builtin_amdgcn_fmed3f(__builtin_rintf(mx_clean(v[e], inv)), -127.0f, 127.0f);
+}
+// The codes of a vector of y, n values of it, at channel `at` of a row: int8 with the row's step.
+__device__ __forceinline__ void put_int8(const Args& a, int64_t row, int at, int n, const float (&v)[kVec], float inv) {
+  uint8_t c[kVec];
+  int8_codes(v, inv, c);
   uint8_t* p = a.codes + row * a.D + at;
   if (n == kVec) {
     __builtin_memcpy(p, c, kVec);
@@ -68,8 +71,8 @@ __device__ __forceinline__ uint32_t biggest_of(const float (&v)[kVec], uint32_t 
   return big;
 }
 
-// kGroups: several groups of a width that is a multiple of eight.
-template <typename T, bool kWave, int kMost, int kThreads, bool kGroups>
+// kGroups: several groups of a width that is a multiple of eight.  kMost vectors of every thread, all whole.
+template <typename T, bool kWave, int kMost, int kThreads, bool kGroups, bool kZ, bool kR>
 __global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int walk) {
   extern __shared__ float terms_all[];
   __shared__ float part[2][16];
@@ -86,62 +89,80 @@ __global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int wal
     else __syncthreads();
   };
 
-  int at[kMost], n[kMost];   // a vector's first channel, and how many of its values the row has
+  int at[kMost];   // a vector's first channel
   float w[kMost][kVec];
 #pragma unroll
   for (int i = 0; i < kMost; ++i) {
     at[i] = (i * threads + t) * kVec;
-    n[i] = a.D - at[i] < 0 ? 0 : a.D - at[i] < kVec ? a.D - at[i] : kVec;
-    if (n[i] > 0) load_vec<float>(a.w + at[i], n[i], w[i]);
+    if (at[i] < a.D) load_vec<float>(a.w + at[i], kVec, w[i]);
   }
   RawVec<T> x[kMost], z[kMost], r[kMost];
-  auto request = [&](RawVec<T>& v, const void* p, int64_t off, int m) {
-    if (m == kVec) {
-      __builtin_memcpy(&v, static_cast<const T*>(p) + off, sizeof(v));
-    } else {
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) v.v[e] = e < m ? static_cast<const T*>(p)[off + e] : (T)0.0f;
-    }
-  };
+  auto request = [&](RawVec<T>& v, const void* p, int64_t off) { __builtin_memcpy(&v, static_cast<const T*>(p) + off, sizeof(v)); };
   auto fetch = [&](int64_t row) {
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
-      if (n[i] <= 0) continue;
-      request(x[i], a.x, row * a.x_row + at[i], n[i]);
-      if (a.z) request(z[i], a.z, row * a.z_row + at[i], n[i]);
-      if (a.residual) request(r[i], a.residual, row * a.D + at[i], n[i]);
+      if (at[i] >= a.D) continue;
+      request(x[i], a.x, row * a.x_row + at[i]);
+      if constexpr (kZ) request(z[i], a.z, row * a.z_row + at[i]);
+      if constexpr (kR) request(r[i], a.residual, row * a.D + at[i]);
     }
+  };
+  // A row's results are stored behind the next row's loads: loads and stores count down in one order, and the wait for
+  // the loads, had it the stores before it, would be for those too.
+  const int row_vecs = a.blocks * (kMxBlock / kVec);
+  RawVec<T> sums[kMost];
+  uint2 codes[kMost];
+  uint32_t scales[kMost];
+  float step = 0.0f;
+  auto put = [&](int64_t row) {
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      if (kR && at[i] < a.D) __builtin_memcpy(static_cast<T*>(a.residual_out) + row * a.D + at[i], &sums[i], sizeof(sums[i]));
+      if (a.format == SSDI8_FMT_I8) {
+        if (at[i] < a.D) __builtin_memcpy(a.codes + row * a.D + at[i], &codes[i], 8);
+      } else if (at[i] < row_vecs * kVec) {
+        const int64_t o = row * row_vecs + at[i] / kVec;
+        if (a.format == SSDI8_FMT_MXFP8) __builtin_memcpy(a.codes + o * kVec, &codes[i], 8);
+        else __builtin_memcpy(a.codes + o * (kVec / 2), &codes[i], 4);
+        if ((t & 3) == 0) a.scales[o / 4] = (uint8_t)scales[i];
+      }
+    }
+    if (a.format == SSDI8_FMT_I8 && t == 0) reinterpret_cast<float*>(a.scales)[row] = step;
   };
   fetch(row0);
   for (int64_t row = row0; row < row1; ++row) {
     const int turn = (int)(row - row0) & 1;   // a wave may be a row behind another, not two
     float v[kMost][kVec], g[kMost][kVec];
     float sum = 0.0f;
+    // every value of this row is here: said for all lanes, those without a vector too
+    __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0)
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
-      if (n[i] <= 0) continue;
+      if (at[i] >= a.D) continue;
 #pragma unroll
-      for (int e = 0; e < kVec; ++e) v[i][e] = (float)x[i].v[e];
-      if (a.residual) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) v[i][e] += (float)r[i].v[e];
-        store_vec<T>(static_cast<T*>(a.residual_out) + row * a.D + at[i], n[i], v[i]);
-      }
-      if (a.z) {
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) g[i][e] = silu((float)z[i].v[e]);
-        if (!a.before)
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) v[i][e] *= g[i][e];
+      for (int e = 0; e < kVec; ++e) {
+        v[i][e] = (float)x[i].v[e];
+        if constexpr (kR) v[i][e] += (float)r[i].v[e];
+        if constexpr (kZ) g[i][e] = silu((float)z[i].v[e]);
       }
     }
+    if (row > row0) put(row - 1);
     if (row + 1 < row1) fetch(row + 1);
+#pragma unroll
+    for (int i = 0; i < kMost; ++i) {
+      if (at[i] >= a.D) continue;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        if constexpr (kR) sums[i].v[e] = (T)v[i][e];
+        if constexpr (kZ) v[i][e] = a.before ? v[i][e] : v[i][e] * g[i][e];
+      }
+    }
     if constexpr (!kGroups) {
 #pragma unroll
       for (int i = 0; i < kMost; ++i) {
-        if (n[i] <= 0) continue;
+        if (at[i] >= a.D) continue;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) sum = __builtin_fmaf(v[i][e], v[i][e], sum);   // 0 behind the row's end
+        for (int e = 0; e < kVec; ++e) sum = __builtin_fmaf(v[i][e], v[i][e], sum);
       }
       sum = lane_sum<64>(sum);
       if constexpr (!kWave) {
@@ -155,7 +176,7 @@ __global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int wal
       if (row > row0) meet();   // the last row's scales are read
 #pragma unroll
       for (int i = 0; i < kMost; ++i) {
-        if (n[i] <= 0) continue;
+        if (at[i] >= a.D) continue;
         float s = 0.0f;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) s = __builtin_fmaf(v[i][e], v[i][e], s);
@@ -175,22 +196,16 @@ __global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int wal
     uint32_t big = 0;
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
-      if (n[i] <= 0) {
+      const bool own = at[i] < a.D;
+      const float scale = kGroups ? terms[own ? at[i] / a.width * (a.width / kVec) : 0] : sum;
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[i][e] = 0.0f;   // behind the row's end, up to a whole block
-        continue;
+      for (int e = 0; e < kVec; ++e) {
+        float u = v[i][e] * scale * w[i][e];
+        if constexpr (kZ) u = a.before ? u * g[i][e] : u;
+        v[i][e] = own ? u : 0.0f;   // behind the row's end, up to a whole block: 0
       }
-      const float scale = kGroups ? terms[at[i] / a.width * (a.width / kVec)] : sum;
-#pragma unroll
-      for (int e = 0; e < kVec; ++e) v[i][e] = v[i][e] * scale * w[i][e];
-      if (a.z && a.before)
-#pragma unroll
-        for (int e = 0; e < kVec; ++e) v[i][e] *= g[i][e];
-#pragma unroll
-      for (int e = 0; e < kVec; ++e)
-        if (e >= n[i]) v[i][e] = 0.0f;   // 0 times a scale that is no number
       big = biggest_of(v[i], big);
-      if (a.y) store_vec<T>(static_cast<T*>(a.y) + row * a.D + at[i], n[i], v[i]);
+      if (a.y && own) store_vec<T>(static_cast<T*>(a.y) + row * a.D + at[i], kVec, v[i]);
     }
     if (a.format == SSDI8_FMT_I8) {
       big = wave_max(big);
@@ -201,16 +216,28 @@ __global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int wal
         for (int i = 0; i < threads / 64; ++i) big = big > biggest[turn][i] ? big : biggest[turn][i];
       }
       float inv;
-      const float step = int8_step(big, inv);
+      step = int8_step(big, inv);
 #pragma unroll
-      for (int i = 0; i < kMost; ++i)
-        if (n[i] > 0) put_int8(a, row, at[i], n[i], v[i], inv);
-      if (t == 0) reinterpret_cast<float*>(a.scales)[row] = step;
+      for (int i = 0; i < kMost; ++i) {
+        uint8_t c[kVec];
+        int8_codes(v[i], inv, c);
+        __builtin_memcpy(&codes[i], c, kVec);
+      }
     } else {
 #pragma unroll
-      for (int i = 0; i < kMost; ++i) put_blocks(a, row, at[i], v[i]);
+      for (int i = 0; i < kMost; ++i) {
+        const uint32_t block = quad_max(biggest_of(v[i], 0));
+        if (a.format == SSDI8_FMT_MXFP8) {
+          scales[i] = mx_scale<SSDI8_FMT_MXFP8>(block);
+          codes[i] = mx_e4m3(v[i], mx_inverse(scales[i]));
+        } else {
+          scales[i] = mx_scale<SSDI8_FMT_MXFP4>(block);
+          codes[i].x = mx_e2m1(v[i], mx_inverse(scales[i]));
+        }
+      }
     }
   }
+  put(row1 - 1);
 }
 
 // A row's values in LDS, a workgroup for each row.
@@ -316,7 +343,7 @@ template <typename T> __global__ __launch_bounds__(1024) void norm_quantize_lds_
 template <typename T> hipError_t run(const Args& a, hipStream_t st) {
   // Threads for the row's whole blocks, too.
   const int vecs = a.blocks * (kMxBlock / kVec);
-  if (vecs > 1024 || (a.groups > 1 && a.width % kVec != 0)) {
+  if (vecs > 1024 || a.D % kVec != 0 || a.width % kVec != 0) {
     const int threads = vecs < 1024 ? (vecs + 63) / 64 * 64 : 1024;
     const size_t lds = sizeof(float) * a.D;
     if (lds > 64 * 1024) {   // more than a kernel may have unasked
@@ -335,9 +362,14 @@ template <typename T> hipError_t run(const Args& a, hipStream_t st) {
     while (walk < 4 && a.rows / (2 * walk) >= 2048 * kItems) walk *= 2;
     const int64_t count = (a.rows + walk - 1) / walk;
     const size_t lds = kGroups ? sizeof(float) * kItems * (a.D / kVec) : 0;
-    norm_quantize_kernel<T, kWave, decltype(most)::value, decltype(limit)::value, kGroups>
-        <<<dim3((unsigned)((count + kItems - 1) / kItems)), threads, lds, st>>>(a, walk);
-    return hipGetLastError();
+    auto go = [&](auto z, auto r) {
+      norm_quantize_kernel<T, kWave, decltype(most)::value, decltype(limit)::value, kGroups, decltype(z)::value,
+                           decltype(r)::value>
+          <<<dim3((unsigned)((count + kItems - 1) / kItems)), threads, lds, st>>>(a, walk);
+      return hipGetLastError();
+    };
+    if (a.residual) return a.z ? go(std::true_type(), std::true_type()) : go(std::false_type(), std::true_type());
+    return a.z ? go(std::true_type(), std::false_type()) : go(std::false_type(), std::false_type());
   };
   using std::integral_constant;
   auto by_width = [&](auto groups) {

@@ -7,19 +7,28 @@ namespace ssdi8 {
 
 namespace {
 
+// A thread takes vectors kStep apart, kUnroll of them on their way at once.
+constexpr int kUnroll = 4;
+
 template <typename T, int kFormat>
 __global__ __launch_bounds__(256) void quantize_mx_kernel(const T* x, int64_t x_row, int64_t rows, int k,
                                                           int row_vecs, uint8_t* codes, uint8_t* scales) {
   constexpr int kBytes = kFormat == SSDI8_FMT_MXFP8 ? kVec : kVec / 2;
   const int64_t total = rows * row_vecs;
-  const int64_t step = (int64_t)gridDim.x * 256;
-  // whole quads walk together: total is a multiple of 4
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+  const int64_t first = (int64_t)blockIdx.x * (256 * kUnroll) + threadIdx.x;
+  float v[kUnroll][kVec];
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t i = first + u * 256;
     const int64_t row = i / row_vecs;
     const int o = (int)(i - row * row_vecs) * kVec;
-    float v[kVec];
-    load_vec<T>(x + row * x_row + o, k - o, v);
-    mx_put<kFormat>(v, codes + i * kBytes, scales + i / 4, true);
+    if (i < total) load_vec<T>(x + row * x_row + o, k - o, v[u]);
+  }
+  // whole quads have a vector: total is a multiple of 4
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u) {
+    const int64_t i = first + u * 256;
+    if (i < total) mx_put<kFormat>(v[u], codes + i * kBytes, scales + i / 4, true);
   }
 }
 
@@ -28,8 +37,7 @@ __global__ __launch_bounds__(256) void quantize_mx_kernel(const T* x, int64_t x_
 hipError_t launch_quantize_mx(int dtype, int format, int64_t rows, int64_t k, const void* x, int64_t x_row,
                               void* codes, void* scales, hipStream_t st) {
   const int row_vecs = (int)(mx_blocks(k) * (kMxBlock / kVec));
-  const int64_t wgs = (rows * row_vecs + 255) / 256;
-  const unsigned grid = (unsigned)(wgs < 256 * 64 ? wgs : 256 * 64);
+  const unsigned grid = (unsigned)((rows * row_vecs + 256 * kUnroll - 1) / (256 * kUnroll));
   auto go = [&](auto t, auto f) {
     typedef decltype(t) T;
     quantize_mx_kernel<T, decltype(f)::value>
