@@ -792,6 +792,17 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Args p) {
   }
 }
 
+// Four values at any alignment of one, past the caches: a state is read and written once.
+typedef float v4f_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ float4 load4(const float* p) {
+  const v4f_any v = __builtin_nontemporal_load(reinterpret_cast<const v4f_any*>(p));
+  return make_float4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ void store4(float* p, float4 f) {
+  const v4f_any v = {f.x, f.y, f.z, f.w};
+  __builtin_nontemporal_store(v, reinterpret_cast<v4f_any*>(p));
+}
+
 // One token.  A workgroup takes 64 columns of a head's state: 16 threads of four columns each, 16 such rows of
 // threads.  Bound by the state's bytes: all of a thread's loads are on their way before the first is used.
 template <typename T, int kRows>
@@ -815,7 +826,7 @@ __global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, 
     if (key >= keys || cols == 0) continue;
     const float* at = state + (int64_t)key * a.values;
     if (cols == 4) {
-      __builtin_memcpy(&s[i], at, 16);
+      s[i] = load4(at);
     } else {
       s[i].x = at[0];
       if (cols > 1) s[i].y = at[1];
@@ -852,7 +863,7 @@ __global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, 
     if (key >= keys || cols == 0) continue;
     float* at = state + (int64_t)key * a.values;
     if (cols == 4) {
-      __builtin_memcpy(at, &s[i], 16);
+      store4(at, s[i]);
     } else {
       at[0] = s[i].x;
       if (cols > 1) at[1] = s[i].y;

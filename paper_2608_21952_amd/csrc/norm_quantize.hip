@@ -357,7 +357,8 @@ template <typename T> hipError_t run(const Args& a, hipStream_t st) {
   auto launch = [&](auto wave, auto most, auto limit, auto groups, int threads) {
     constexpr bool kWave = decltype(wave)::value, kGroups = decltype(groups)::value;
     constexpr int kItems = kWave ? 4 : 1;
-    // rows of a walk: as many as leave every CU eight workgroups, four at most
+    // rows of a walk: as many as leave every CU eight workgroups, four at most (16384 x 5120 with gate: 109 us at two,
+    // 104 at four and eight; 16384 x 2560 with residual 53, 49, 54)
     int walk = 1;
     while (walk < 4 && a.rows / (2 * walk) >= 2048 * kItems) walk *= 2;
     const int64_t count = (a.rows + walk - 1) / walk;
@@ -378,7 +379,8 @@ template <typename T> hipError_t run(const Args& a, hipStream_t st) {
     using W = integral_constant<int, 256>;
     if (vecs <= 64) return launch(std::true_type(), One(), W(), groups, 256);
     if (vecs <= 128) return launch(std::true_type(), Two(), W(), groups, 256);
-    return launch(std::false_type(), Two(), integral_constant<int, 512>(), groups, (vecs + 127) / 128 * 64);
+    // A vector per thread: two of them left half as many waves (16384 x 5120 with gate 118 us, 104 with one).
+    return launch(std::false_type(), One(), integral_constant<int, 1024>(), groups, (vecs + 63) / 64 * 64);
   };
   return a.groups == 1 ? by_width(std::false_type()) : by_width(std::true_type());
 }
