@@ -8,9 +8,12 @@
 // an instruction is free.  A k-tile is eight blocks: half h takes blocks 4 h + s in step s, so that a lane's four
 // scales are the four bytes of one word.
 //
-// Many rows (mx_tile): a workgroup forms a kBM x kBN tile of y from k-tiles in two LDS buffers, the next one on its way
+// Many rows (mx_tile): a workgroup forms a kBM x kBN tile of y from k-tiles in two LDS buffers, a third one on its way
 // in registers.  LDS holds 16-byte chunk c of a line (128 bytes) of row r at slot c ^ (r / 2 % 8), so that the
 // 16 lanes that a fragment read serves at a time touch every bank once.
+// What bounds it: the way of the operands into LDS (a tile of 128 x 128 needs 32 KB for 512 cycles of a SIMD's products)
+// and the way out; 16384 x 10496 x 2560 395 us (2.2 PFLOP/s, the vendor's library 456; products from registers alone
+// reach 5.7), with e4m3 x 508 (library, both operands e4m3, 775).  Tiles of 256 x 256 did not fit the registers.
 // Few rows (mx_rows): bound by the bytes of w.  A workgroup takes 16 rows of w, its waves share k by lines of 128
 // bytes, each straight from memory into the matrix instruction's registers, and their sums meet in LDS.
 #include "common.hpp"
@@ -109,104 +112,155 @@ __global__ __launch_bounds__(64 * kWM * kWN) void mx_tile(LinearMx a, int mtiles
   constexpr int kA = kBM * kXL / kLoadLines, kB = kBN / kLoadLines, kParts = kA + kB;
   static_assert(kLoadLines % 16 == 0 && kBM % kLoadLines == 0 && kBN % kLoadLines == 0, "tile");
   const int lrow = tid / 8, chunk = (tid % 8) ^ slot_key(lrow);
-  // rows behind the last are taken for it: their results are not stored
-  uint32_t offset[kParts];
-#pragma unroll
-  for (int i = 0; i < kParts; ++i) {
-    const int64_t left = i < kA ? a.m - m0 : a.n - n0;
-    int64_t r = i < kA ? (i * kLoadLines + lrow) % kBM : (i - kA) * kLoadLines + lrow;
-    r = r < left ? r : left - 1;
-    offset[i] = (uint32_t)(r * (i < kA ? x_row : w_row)) + chunk * 16 + (i < kA ? (i * kLoadLines) / kBM * kLine : 0);
-  }
-  const char* xp = reinterpret_cast<const char*>(a.x) + m0 * x_row;
-  const char* wp = reinterpret_cast<const char*>(a.w) + n0 * w_row;
+  // One offset for all loads, the rest in scalar registers; rows behind the last give 0, as what lies at kNowhere does.
+  constexpr uint32_t kNowhere = 0xfffffff0u;
+  auto tile_of = [](const uint8_t* p, int64_t row, int64_t rows, int64_t row_bytes) {
+    const int64_t bytes = (rows - row) * row_bytes;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p + row * row_bytes), 0,
+                                             (int)(uint32_t)(bytes < 0xffff0000ll ? bytes : 0xffff0000ll), 0x00027000);
+  };
+  const auto x_tile = tile_of(a.x, m0, a.m, x_row), w_tile = tile_of(a.w, n0, a.n, w_row);
+  const uint32_t x_off = (uint32_t)(lrow * x_row) + chunk * 16, w_off = (uint32_t)(lrow * w_row) + chunk * 16;
 
   const int fr = lane & 31, fh = lane >> 5;
-  const uint8_t *xs_row[kTM], *ws_row[kTN];
-#pragma unroll
-  for (int i = 0; i < kTM; ++i) {
-    const int64_t r = m0 + (wm * kTM + i) * 32 + fr;
-    xs_row[i] = a.xs + (r < a.m ? r : a.m - 1) * a.blocks + 4 * fh;
-  }
-#pragma unroll
-  for (int j = 0; j < kTN; ++j) {
-    const int64_t r = n0 + (wn * kTN + j) * 32 + fr;
-    ws_row[j] = a.ws + (r < a.n ? r : a.n - 1) * a.blocks + 4 * fh;
-  }
-
   v16f acc[kTN][kTM] = {};
-  uint4 part[kParts];
-  uint32_t xs[2][kTM], ws[2][kTN];
-  auto request = [&](int kt) {
-#pragma unroll
-    for (int i = 0; i < kParts; ++i) {
-      const int64_t at = (int64_t)kt * (i < kA ? kXL * kLine : kLine);
-      const int64_t in_row = at + chunk * 16 + (i < kA ? (i * kLoadLines) / kBM * kLine : 0);
-      part[i] = make_uint4(0, 0, 0, 0);
-      if (in_row < (i < kA ? x_row : w_row)) __builtin_memcpy(&part[i], (i < kA ? xp : wp) + at + offset[i], 16);
-    }
+  // A lane's scales of a k-tile: the bytes of blocks 4 fh .. 4 fh + 3, one load for each 32 rows.  Rows behind the last
+  // give 0.
+  const int xs0 = wm * kTM * 32, ws0 = wn * kTN * 32;
+  auto rows_of = [](const uint8_t* p, int64_t row, int64_t rows, int64_t blocks) {
+    const int64_t bytes = row < rows ? (rows - row) * blocks : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p + row * blocks), 0,
+                                             (int)(bytes < 0x40000000 ? bytes : 0x40000000), 0x00027000);
   };
-  auto scales = [&](int kt, uint32_t (&sx)[kTM], uint32_t (&sw)[kTN]) {
-    const int64_t b = (int64_t)kt * kTileBlocks;
-#pragma unroll
-    for (int i = 0; i < kTM; ++i) sx[i] = scale_word<4>(xs_row[i], b, a.blocks - 4 * fh);
-#pragma unroll
-    for (int j = 0; j < kTN; ++j) sw[j] = scale_word<4>(ws_row[j], b, a.blocks - 4 * fh);
+  const auto xs_rows = rows_of(a.xs, m0 + xs0, a.m, a.blocks), ws_rows = rows_of(a.ws, n0 + ws0, a.n, a.blocks);
+  const int blocks = (int)a.blocks, s_off = fr * blocks + 4 * fh;
+  struct Scales {
+    uint32_t x[kTM], w[kTN];
   };
-  auto put = [&](int kt) {
-    char* buf = lds + (kt & 1) * kBuf + tid * 16;
+  auto read_scales = [&](int kt, Scales& s) {
+    const int at = s_off + kt * kTileBlocks;
 #pragma unroll
-    for (int i = 0; i < kParts; ++i)
-      *reinterpret_cast<uint4*>(buf + (i < kA ? 0 : kXBytes) + (i < kA ? i : i - kA) * kThreads * 16) = part[i];
+    for (int i = 0; i < kTM; ++i) s.x[i] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(xs_rows, at, i * 32 * blocks, 0);
+#pragma unroll
+    for (int j = 0; j < kTN; ++j) s.w[j] = (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(ws_rows, at, j * 32 * blocks, 0);
   };
-  auto step = [&](int kt, auto s_) {
-    constexpr int s = decltype(s_)::value;
+  // In a row's last k-tile: what lies behind its end is another row's, and may be a NaN; its codes are 0.  Where a word
+  // would end behind the last row's end it is not read: byte by byte.
+  auto cut_scales = [&](int kt, Scales& s) {
+    const int left = blocks - kt * kTileBlocks - 4 * fh;
+    auto word = [&](auto rows, int row) {
+      uint32_t v = 0;
+      for (int e = 0; e < 4 && e < left; ++e)
+        v |= (uint32_t)(uint8_t)__builtin_amdgcn_raw_buffer_load_b8(rows, s_off + kt * kTileBlocks + e, row * blocks, 0) << (8 * e);
+      return v;
+    };
+#pragma unroll
+    for (int i = 0; i < kTM; ++i) s.x[i] = word(xs_rows, i * 32);
+#pragma unroll
+    for (int j = 0; j < kTN; ++j) s.w[j] = word(ws_rows, j * 32);
+  };
+
+  struct Frags {
+    Part<kX> x[kTM];
+    Part<kE2m1> w[kTN];
+  };
+  auto read = [&](int kt, int s, Frags& f) {
     const char* buf = lds + (kt & 1) * kBuf;
-    Part<kX> fx[kTM];
-    Part<kE2m1> fw[kTN];
+    const int w_at = ((4 * fh + s) ^ slot_key(fr)) * 16, x_at = kX == kE4m3 ? ((2 * s + fh) ^ slot_key(fr)) * 16 : w_at;
 #pragma unroll
     for (int i = 0; i < kTM; ++i) {
-      const char* row = buf + (wm * kTM * 32 + i * 32 + fr) * kLine;
-      if constexpr (kX == kE4m3) {
-        const int off = ((2 * s + fh) ^ slot_key(fr)) * 16;
-        fx[i].v[0] = *reinterpret_cast<const uint4*>(row + off);
-        fx[i].v[1] = *reinterpret_cast<const uint4*>(row + kBM * kLine + off);
-      } else {
-        fx[i].v[0] = *reinterpret_cast<const uint4*>(row + ((4 * fh + s) ^ slot_key(fr)) * 16);
-      }
+      const char* row = buf + (xs0 + i * 32 + fr) * kLine + x_at;
+      f.x[i].v[0] = *reinterpret_cast<const uint4*>(row);
+      if constexpr (kX == kE4m3) f.x[i].v[1] = *reinterpret_cast<const uint4*>(row + kBM * kLine);
     }
 #pragma unroll
     for (int j = 0; j < kTN; ++j)
-      fw[j].v[0] = *reinterpret_cast<const uint4*>(buf + kXBytes + (wn * kTN * 32 + j * 32 + fr) * kLine +
-                                                   ((4 * fh + s) ^ slot_key(fr)) * 16);
-#pragma unroll
-    for (int j = 0; j < kTN; ++j)
-#pragma unroll
-      for (int i = 0; i < kTM; ++i)
-        acc[j][i] = mma32<kX, s>(fw[j], ws[0][j], fx[i], xs[0][i], acc[j][i]);
+      f.w[j].v[0] = *reinterpret_cast<const uint4*>(buf + kXBytes + (ws0 + j * 32 + fr) * kLine + w_at);
   };
-  request(0);
-  scales(0, xs[0], ws[0]);
-  put(0);
-  __syncthreads();
-  for (int kt = 0; kt < ktiles; ++kt) {
-    if (kt + 1 < ktiles) {
-      request(kt + 1);
-      scales(kt + 1, xs[1], ws[1]);
-    }
-    step(kt, std::integral_constant<int, 0>());
-    step(kt, std::integral_constant<int, 1>());
-    step(kt, std::integral_constant<int, 2>());
-    step(kt, std::integral_constant<int, 3>());
-    if (kt + 1 < ktiles) {
-      put(kt + 1);
+  // One 16-byte load per lane of a k-tile on its way, and its place in LDS.
+  uint4 part[kParts];
+  auto request = [&](int kt, int i, auto inside) {   // inside: a whole k-tile
+    const bool is_x = i < kA;
+    // rows, and for x lines, from the tile's first on
+    const uint32_t line = is_x ? (uint32_t)(i * kLoadLines / kBM * kLine) : 0u;
+    const uint32_t row = is_x ? (uint32_t)(i * kLoadLines % kBM) * (uint32_t)x_row : (uint32_t)((i - kA) * kLoadLines) * (uint32_t)w_row;
+    const uint32_t at = (uint32_t)kt * (uint32_t)(is_x ? kXL * kLine : kLine) + line;
+    uint32_t off = is_x ? x_off : w_off;
+    if constexpr (!decltype(inside)::value) off = at + chunk * 16 < (uint32_t)(is_x ? x_row : w_row) ? off : kNowhere;
+    part[i] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(is_x ? x_tile : w_tile, (int)off, (int)(row + at), 0));
+  };
+  auto put = [&](int kt, int i) {
+    char* buf = lds + (kt & 1) * kBuf + tid * 16;
+    *reinterpret_cast<uint4*>(buf + (i < kA ? 0 : kXBytes) + (i < kA ? i : i - kA) * kThreads * 16) = part[i];
+  };
+  // Step s of k-tile kt forms the products of 64 values.  Meanwhile the next step's fragments are read, over the
+  // k-tiles' borders too, and the next k-tile moves from registers to the other buffer, a part per step, each part's
+  // registers taking the k-tile after it.
+  constexpr int kSteps = 4, kPerStep = (kParts + kSteps - 2) / (kSteps - 1);
+  Frags f[2];
+  Scales sc[2];
+  auto begin = [&](auto inside) {
 #pragma unroll
-      for (int i = 0; i < kTM; ++i) xs[0][i] = xs[1][i];
+    for (int i = 0; i < kParts; ++i) request(0, i, inside);
+    read_scales(0, sc[0]);
 #pragma unroll
-      for (int j = 0; j < kTN; ++j) ws[0][j] = ws[1][j];
-    }
+    for (int i = 0; i < kParts; ++i) put(0, i);
+    if (decltype(inside)::value || ktiles > 1)
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) request(1, i, inside);
     __syncthreads();
+    read(0, 0, f[0]);
+  };
+  auto k_tile = [&](int kt, auto inside) {   // inside: k-tiles kt + 1 and kt + 2 are there and whole
+    constexpr bool kInside = decltype(inside)::value;
+    const Scales now = sc[0];
+    auto step = [&](auto s_) {
+      constexpr int s = decltype(s_)::value;
+      if (s + 1 < kSteps) {
+        read(kt, s + 1, f[(s + 1) & 1]);
+      } else if (kInside || kt + 1 < ktiles) {
+        __syncthreads();   // the next buffer is written, this one read
+        read(kt + 1, 0, f[0]);
+      }
+      if (s == 0 && (kInside || kt + 1 < ktiles)) read_scales(kt + 1, sc[0]);
+#pragma unroll
+      for (int j = 0; j < kTN; ++j) {
+#pragma unroll
+        for (int i = 0; i < kTM; ++i)
+          acc[j][i] = mma32<kX, s>(f[s & 1].w[j], now.w[j], f[s & 1].x[i], now.x[i], acc[j][i]);
+        // the compiler would otherwise gather the loads at the end of the k-tile
+        __builtin_amdgcn_sched_barrier(0);
+        if (j == 0 && s + 1 < kSteps && (kInside || kt + 1 < ktiles)) {
+#pragma unroll
+          for (int e = 0; e < kPerStep; ++e) {
+            const int i = s * kPerStep + e;
+            if (i < kParts) {
+              put(kt + 1, i);
+              if (kInside || kt + 2 < ktiles) request(kt + 2, i, inside);
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    };
+    step(std::integral_constant<int, 0>());
+    step(std::integral_constant<int, 1>());
+    step(std::integral_constant<int, 2>());
+    step(std::integral_constant<int, 3>());
+  };
+  const int whole = (int)(a.blocks / kTileBlocks);   // k-tiles
+  int kt = 0;
+  if (whole > 2) {
+    begin(std::true_type());
+    for (; kt + 2 < whole; ++kt) k_tile(kt, std::true_type());
+  } else {
+    begin(std::false_type());
   }
+  for (; kt < ktiles; ++kt) {
+    if (kt >= whole) cut_scales(kt, sc[0]);
+    k_tile(kt, std::false_type());
+  }
+  __syncthreads();
 
   // a lane holds row fr of the 32 x 32 block, columns 8 q + 4 fh + (0..3); on the way out it has eight columns
   float* out = reinterpret_cast<float*>(lds) + wave * 32 * kOutRow;
@@ -228,7 +282,7 @@ __global__ __launch_bounds__(64 * kWM * kWN) void mx_tile(LinearMx a, int mtiles
             make_float4(acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]);
     // the wave's own rows: no other wave reads or writes them
     __builtin_amdgcn_wave_barrier();
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < 32 * kPer / 64; ++k) {
       const int r = (k * 64 + lane) / kPer;
       const int64_t mm = wm0 + i * 32 + r;
@@ -345,12 +399,27 @@ template <int kX, int kBM, int kBN, int kWM, int kWN> hipError_t run_tile(const 
   return hipGetLastError();
 }
 
+template <int kX> hipError_t by_tiles(const LinearMx& a, hipStream_t st) {
+  auto count = [&](int64_t bm, int64_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
+  // Small tiles where large ones leave CUs without work: us with 64 x 64 / 128 x 128 e2m1 512 x 5120 x 2560 12.6 / 12.8,
+  // 1000 x 2900 x 992 10.3 / 10.7, 2048 x 2560 x 5120 42.3 / 38.4; e4m3 with 128 x 256 15.2 / 22.0, 11.1 / 16.3, 49.6 / 42.9.
+  if constexpr (kX == kE4m3) {
+    if (count(128, 256) < 128) return run_tile<kX, 64, 64, 2, 2>(a, st);
+    return run_tile<kX, 128, 256, 2, 4>(a, st);
+  } else {
+    if (count(128, 128) < 256) return run_tile<kX, 64, 64, 2, 2>(a, st);
+    // Eight waves where a tile's way out is much of its time, four (more products per value read from LDS) over a long k:
+    // 16384 x 10496 x 2560 395 / 469, 16384 x 768 x 1536 24 / 28, 16384 x 2560 x 5120 210 / 179, 2048 x 2560 x 5120 45 / 38.
+    if (a.blocks >= 128) return run_tile<kX, 128, 128, 2, 2>(a, st);
+    return run_tile<kX, 128, 128, 2, 4>(a, st);
+  }
+}
+
 template <int kX> hipError_t run(const LinearMx& a, hipStream_t st) {
   const unsigned strips = (unsigned)((a.n + 15) / 16);
   if (a.m <= 16) mx_rows<kX, 1, 8><<<strips, 512, 0, st>>>(a);
   else if (a.m <= 32) mx_rows<kX, 2, 8><<<strips, 512, 0, st>>>(a);
-  else if (((a.m + 127) / 128) * ((a.n + 127) / 128) >= 256) return run_tile<kX, 128, 128, 2, 2>(a, st);
-  else return run_tile<kX, 64, 64, 2, 2>(a, st);
+  else return by_tiles<kX>(a, st);
   return hipGetLastError();
 }
 

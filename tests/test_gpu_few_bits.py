@@ -255,6 +255,26 @@ def test_linear_mx_is_a_sum_of_integers(ssdi8, M, format):
     assert torch.equal(got.cpu().double(), x.double() @ w.double().T)
 
 
+# Sizes that take the large tiles, each with a last tile and a last k-tile that are cut.
+@pytest.mark.parametrize("format", ["mxfp8", "mxfp4"])
+@pytest.mark.parametrize("M,O,K,act,bias,residual,ydt", [(2107, 2011, 992, "gelu", True, True, F16),
+                                                         (2107, 2011, 4128, None, False, False, F32),
+                                                         (4001, 1100, 32, "silu", True, False, BF16)])
+def test_linear_mx_large(ssdi8, M, O, K, act, bias, residual, ydt, format):
+    test_linear_mx(ssdi8, M, O, K, act, bias, residual, ydt, format)
+
+
+@pytest.mark.parametrize("format", ["mxfp8", "mxfp4"])
+@pytest.mark.parametrize("K", [1312, 4192])
+def test_linear_mx_large_is_a_sum_of_integers(ssdi8, K, format):
+    g = gen(K)
+    w = torch.randint(-3, 4, (2050, K), generator=g).float()
+    x = torch.randint(-3, 4, (2080, K), generator=g).float()
+    w[:, ::32], x[:, ::32] = 4.0, 4.0
+    W, X = ssdi8.quantize_mx(w.cuda()), ssdi8.quantize_mx(x.cuda(), format)
+    assert torch.equal(ssdi8.linear_mx(X, W, y_dtype=F32).double(), x.cuda().double() @ w.cuda().double().T)
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("format", ["mxfp8", "mxfp4"])
 @pytest.mark.parametrize("M,K", [(5, 1000), (90, 512)])
