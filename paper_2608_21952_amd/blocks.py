@@ -6,6 +6,7 @@ gate, output projection with the residual; over prompts of any length and for si
     x = block.step(x_token, cache)         # (B, d); the cache is updated in place
 
 Weights are a dict of device tensors: projections fp16 (outputs, inputs), everything else fp32.
+LinearAttentionBlock holds its state by linear attention and takes its projections in few bits from the norms.
 """
 from __future__ import annotations
 
@@ -156,3 +157,85 @@ class MambaBlock:
         y = ssdi8.selective_scan_step(*self._selective(u), cache["state"], D=self.w["D"], z=z,
                                       dt_bias=self.w["dt_bias"])
         return self.out_proj(y, residual=x)
+
+
+class NormedProjection:
+    """A projection behind the norm that quantizes its input: int8 with a step per row and per output, or weights in
+    mxfp4 and inputs in mxfp8 or mxfp4; without a format all in fp16.
+
+    norm gives the projection's input from a norm's arguments; with with_y also y in x's type."""
+
+    def __init__(self, weight: torch.Tensor, format: Optional[str] = None):
+        if format not in (None, "int8", "mxfp8", "mxfp4"):
+            raise ValueError(f"format must be None, int8, mxfp8 or mxfp4, got {format!r}")
+        self.format = format
+        if format in (None, "int8"):
+            p = Projection(weight, format == "int8")
+            self.weight, self.scale = p.weight, p.scale
+        else:
+            self.weight, self.scale = ssdi8.quantize_mx(weight), None
+
+    def norm(self, x: torch.Tensor, weight: torch.Tensor, *, with_y: bool = False, **kw) -> Dict[str, torch.Tensor]:
+        if self.format is None:
+            return ssdi8.gated_norm(x, weight, **kw)
+        return ssdi8.norm_quantize(x, weight, format=self.format, with_y=with_y, **kw)
+
+    def __call__(self, n: Dict[str, torch.Tensor], **kw) -> torch.Tensor:
+        if self.format is None:
+            return ssdi8.linear(n["y"], self.weight, **kw)
+        if self.format == "int8":
+            return ssdi8.linear(n["codes"], self.weight, x_scale=n["scales"], w_scale=self.scale, **kw)
+        return ssdi8.linear_mx(ssdi8.Mx(n["codes"], n["scales"]), self.weight, **kw)
+
+
+class LinearAttentionBlock:
+    """Norm, projection to q, k, v and a gate, linear attention with a decay per head, gated norm per head, output
+    projection with the residual.  Activations are fp16, the state (B, v_heads, keys, values) fp32.
+
+    weights: norm (d), in_proj (heads * keys + key_heads * keys + v_heads * values + H * values, d) for q, k, v, the gate, with
+    H = max(heads, v_heads), gate_norm (H * values), out_proj (d, H * values), and the decays: log_decay (v_heads), at
+    most 0, or, per token, decay_proj (v_heads, d) and decay_bias, of which -softplus is taken.
+    key_heads, v_heads: heads unless given.  format: that of the projections (NormedProjection)."""
+
+    def __init__(self, weights: Dict[str, torch.Tensor], *, heads: int, keys: int, values: int,
+                 key_heads: Optional[int] = None, v_heads: Optional[int] = None, format: Optional[str] = None,
+                 eps: float = 1e-5):
+        self.w, self.K, self.V, self.eps = weights, keys, values, eps
+        self.heads = (heads, key_heads or heads, v_heads or heads)
+        self.H = max(heads, self.heads[2])
+        rows = (heads + self.heads[1]) * keys + (self.heads[2] + self.H) * values
+        if weights["in_proj"].shape[0] != rows:
+            raise ValueError(f"in_proj must have {rows} outputs, got {weights['in_proj'].shape[0]}")
+        self.in_proj = NormedProjection(weights["in_proj"], format)
+        self.out_proj = NormedProjection(weights["out_proj"], format)
+
+    def _front(self, x):
+        per_token = "decay_proj" in self.w
+        n = self.in_proj.norm(x, self.w["norm"], eps=self.eps, with_y=per_token)
+        p, at, out = self.in_proj(n), 0, []
+        for heads, width in zip(self.heads, (self.K, self.K, self.V)):
+            out.append(p[..., at:at + heads * width].unflatten(-1, (heads, width)))
+            at += heads * width
+        decay = self.w.get("log_decay")
+        if per_token:
+            decay = ssdi8.linear(n["y"], self.w["decay_proj"], bias=self.w["decay_bias"], activation="softplus",
+                                 y_dtype=torch.float32).neg_()
+        return (*out, decay), p[..., at:]
+
+    def _back(self, y, z, x):
+        n = self.out_proj.norm(y.flatten(-2), self.w["gate_norm"], z=z, eps=self.eps, groups=self.H)
+        return self.out_proj(n, residual=x)
+
+    def prefill(self, x: torch.Tensor, cache: Optional[Dict[str, torch.Tensor]] = None,
+                lengths: Optional[torch.Tensor] = None
+                ) -> Tuple[torch.Tensor, Dict[str, torch.Tensor]]:
+        """lengths: the sequences' own lengths in a batch padded to one; the cache is that of their ends."""
+        x = x.contiguous()
+        qkv, z = self._front(x)
+        a = ssdi8.linear_attention(*qkv, init_state=(cache or {}).get("state"), lengths=lengths)
+        return self._back(a["y"], z, x), {"state": a["final_state"]}
+
+    def step(self, x: torch.Tensor, cache: Dict[str, torch.Tensor]) -> torch.Tensor:
+        x = x.contiguous()
+        qkv, z = self._front(x)
+        return self._back(ssdi8.linear_attention_step(*qkv[:3], cache["state"], qkv[3]), z, x)
