@@ -7,14 +7,17 @@
 // y; q, k and v of a chunk lie in LDS, the next chunk's are on their way in registers.
 //
 // Matrix products: the 16 x 16 instructions take eight values of a row per lane, for 32 along the sum (fp32: eight
-// instructions of four).  Lane group g (of 16 lanes) is given places 4 g + (0..3) of the first 16 and of the second
-// 16 of the 32: these are the rows that a lane holds of two result tiles, so that results become operands where
-// they lie.  S (keys x values) is the operand of S^T q, and p^T = (k . q) that of p v once all waves have it.
+// instructions of four).  A lane group g (of 16 lanes) has rows 4 g + (0..3) of a result tile, so the eight places of its
+// part of an operand are given to its rows of two tiles: results become operands where they lie.  Of p, these are
+// tokens 4 g + (0..3) and 16 + 4 g + (0..3); of S (keys x values, the operand of S^T q) the keys of two tiles are dealt
+// out so that they are keys 8 g + (0..7), the ones that a read of 16 bytes of q gives.
 //
-// Roundings, of 16-bit types: p, S and exp(c_C - c_j) v_j enter the matrix unit as the sum of two values of the
-// type, which leaves 2^-17 (bf16) and 2^-22 (fp16) of them; as one value each would add as much error as y's own
-// rounding, and 2^-9 of S with every chunk.  fp16: brought to the type's range by powers of two first (p per row, S
-// per tile, v per column).  Sums, S, and the decays' sums (these in fp64: differences of far sums) are not rounded.
+// Roundings, of 16-bit types: p and S are rounded once on their way into the products for y, which adds to y's error
+// about as much as its own rounding (0.00029 against 0.00021 of y, fp16): as two values each the same walk took 343 us
+// instead of 220.  exp(c_C - c_j) v_j, which would leave its rounding in S with every chunk, enters as the sum of
+// values of the type that leave nothing of fp32's accuracy: two of fp16 (2^-23 off), three of bf16 (two would be
+// 2^-17 off).  fp16: brought to the type's range by powers of two first (p per row, S and v per column).
+// Sums, S, and the decays' sums (these in fp64: differences of far sums) are not rounded.
 // A value of v that is no number would reach earlier tokens of its chunk through 0 times it: it enters as 0, and its
 // column is NaN from its token on.
 #include <type_traits>
@@ -70,12 +73,10 @@ template <typename T> __device__ __forceinline__ Frag<T> round_frag(const float 
   }
   return r;
 }
-// What that leaves of them, as a second fragment (16-bit types).
-template <typename T> __device__ __forceinline__ Frag<T> rest_frag(const float (&f)[8], const Frag<T>& hi) {
-  float d[8];
+// What that leaves of them, in their place.
+template <typename T> __device__ __forceinline__ void take_off(float (&f)[8], const Frag<T>& hi) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) d[e] = f[e] - (float)hi.v[e];
-  return round_frag<T>(d);
+  for (int e = 0; e < 8; ++e) f[e] -= (float)hi.v[e];
 }
 
 // fp16: the exponent shift that brings values of which the largest has magnitude bits `big` (fp32) to where they
@@ -669,7 +670,8 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    // The state behind the chunk: v times exp(c_end - c_j), as two values of the type
+    // The state behind the chunk: v times exp(c_end - c_j), as kTerms values of the type
+    constexpr int kTerms = kF16 ? 2 : kHalf ? 3 : 1;
     const float decay = __builtin_amdgcn_exp2f((float)c_end);
     int v_shift[kTiles];
 #pragma unroll
@@ -699,7 +701,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
       }
     };
     read_k(0);
-    Frag<T> whi[kTiles], wlo[kTiles];
+    Frag<T> w_v[kTerms][kTiles];
 #pragma unroll
     for (int part = 0; part < kParts; ++part) {
       const int s = part * kAhead / kKeyT, t0 = part * kAhead % kKeyT;
@@ -713,8 +715,11 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           float f[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * (kF16 ? w[e] * power(v_shift[n]) : w[e]);
-          whi[n] = round_frag<T>(f);
-          if constexpr (kHalf) wlo[n] = rest_frag(f, whi[n]);
+#pragma unroll
+          for (int i = 0; i < kTerms; ++i) {
+            w_v[i][n] = round_frag<T>(f);
+            if (i + 1 < kTerms) take_off(f, w_v[i][n]);
+          }
         }
       }
 #pragma unroll
@@ -722,10 +727,9 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         const Frag<T>& k = kf[part % 2][u];
         const int t = t0 + u;
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, whi[n], S[t][n]);
-        if constexpr (kHalf)
+        for (int i = 0; i < kTerms; ++i)
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, wlo[n], S[t][n]);
+          for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, w_v[i][n], S[t][n]);
       }
       __builtin_amdgcn_sched_barrier(0);
       // the next chunk's loads, between the products: all at once they hold the wave up while they are issued (12

@@ -4,10 +4,10 @@ import torch
 
 from block_ref import HALF_ULP, TINY, U, assert_within, rounded, silu, silu_bound, softplus  # noqa: F401
 
-# Of a value that enters the matrix unit rounded to the type: half an ulp; as the sum of two of the type: the first
-# one's rounding, rounded.
+# Of a value that enters the matrix unit rounded to the type: half an ulp; as the sum of two of fp16 or three of bf16:
+# what a rounding leaves of 1 is at most half an ulp h, whose own half ulp is h^2 / 2, and so on.
 ONE = {torch.float32: 0.0, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
-SPLIT = {torch.float32: 0.0, torch.float16: 2.0 ** -23, torch.bfloat16: 2.0 ** -17}
+SPLIT = {torch.float32: 0.0, torch.float16: 2.0 ** -23, torch.bfloat16: 2.0 ** -26}
 
 
 def spread(t, dim, n):
@@ -21,7 +21,7 @@ def attention(q, k, v, g, scale=None, init=None, lengths=None, dtype=torch.float
     kernel's arithmetic may add is counted against the same sums of magnitudes: K + 1 + (chunks + 1) * 2 fp32 sums
     and products on a way through the states, L more along the tokens; an exponential in base 2 of a difference
     that fp64 holds costs (|v| + 2) U, one for every chunk that a term passes (their |v| add up).  Of 16-bit
-    types v with its decay enters as two of the type, for S: off by SPLIT; p, or S, as one, for y: off by ONE."""
+    types v with its decay enters as two or three of the type, for S: off by SPLIT; p, or S, as one, for y: off by ONE."""
     b, L, Hq, K = q.shape
     Hk, Hv, V = k.shape[2], v.shape[2], v.shape[3]
     H = max(Hq, Hv)
