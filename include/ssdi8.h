@@ -499,7 +499,10 @@ ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_
  * init_state and final_state may be the same memory.  With seqlen = 0 q, k, v and y may be NULL.
  * Values that are no numbers: of v, its column of y and of the state are NaN from its token on; of q, k and
  * g, what the formula gives; earlier tokens are not touched.  A decay of exp(-65536) or less is 0.
- * The workspace holds the states of the spans that long sequences of few heads are cut into.
+ * The workspace holds the states of the spans that long sequences of few heads are cut into, and final states on
+ * their way over init_state where several workgroups read that.
+ * 16-bit types: products of rounded operands, so y is off by about its own rounding once more; the state keeps fp32's
+ * accuracy.  64 neighbouring tokens of q, k, v and y span less than 2e9 bytes each (SSDI8_ERR_UNSUPPORTED).
  */
 typedef struct {
   int64_t batch, seqlen, q_heads, k_heads, v_heads, keys, values;

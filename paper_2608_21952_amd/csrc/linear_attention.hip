@@ -152,6 +152,7 @@ struct Args {
   LinearAttention a;
   int slices, spans, chunks, span_chunks;   // column slices of a head; spans of the tokens and their chunks
   int groups;                               // of heads: those that a workgroup takes together
+  float* final_state;
 };
 
 __device__ __host__ __forceinline__ int64_t state_floats(const LinearAttention& a) { return a.keys * a.values; }
@@ -722,6 +723,13 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           }
         }
       }
+      // The next chunk's loads, between the products: all at once they hold the wave up while they are issued (12 of 16
+      // bytes per lane, 1700 to 3000 cycles).  In front of a part's products, so that no branch lies between the last
+      // products and the first use of S: behind one the compiler has left out wait states that such a use needs.
+      if (chunk + 1 < last)
+#pragma unroll
+        for (int piece = part * 3 / kParts; piece < (part + 1) * 3 / kParts; ++piece) request(chunk + 1, piece);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
         const Frag<T>& k = kf[part % 2][u];
@@ -732,11 +740,6 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, w_v[i][n], S[t][n]);
       }
       __builtin_amdgcn_sched_barrier(0);
-      // the next chunk's loads, between the products: all at once they hold the wave up while they are issued (12
-      // of 16 bytes per lane, 1700 to 3000 cycles)
-      if (chunk + 1 < last)
-#pragma unroll
-        for (int piece = part * 3 / kParts; piece < (part + 1) * 3 / kParts; ++piece) request(chunk + 1, piece);
     }
     if constexpr (kF16) {   // without a branch, which would have S in the registers twice
 #pragma unroll
@@ -759,7 +762,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           static_cast<T*>(a.y)[((b * a.seqlen + t) * a.heads + h) * a.values + col0 + col] = (T)0.0f;
       }
   }
-  float* to = kOut ? (a.final_state && span == p.spans - 1 && h * a.v_heads % heads == 0 ? a.final_state : nullptr)
+  float* to = kOut ? (p.final_state && span == p.spans - 1 && h * a.v_heads % heads == 0 ? p.final_state : nullptr)
                    : a.workspace + span * states;
   if (to) {
     to += (b * a.v_heads + hv) * state_floats(a) + col0 + my0;
@@ -794,6 +797,10 @@ __global__ __launch_bounds__(256) void attention_join_kernel(Args p) {
       *at = s;
     }
   }
+}
+
+__global__ __launch_bounds__(256) void attention_copy_kernel(const float* from, float* to, int64_t n) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) to[i] = from[i];
 }
 
 // Four values at any alignment of one, past the caches: a state is read and written once.
@@ -929,19 +936,27 @@ Args plan(const LinearAttention& a) {
   return p;
 }
 
-template <typename T, int kKeys, int kTiles, int kHeads> hipError_t run(const Args& p, hipStream_t st) {
+// Whether other workgroups than the one that writes a final state read its initial one.
+bool read_elsewhere(const Args& p) { return p.spans > 1 || p.a.heads > p.a.v_heads; }
+
+template <typename T, int kKeys, int kTiles, int kHeads> hipError_t run(Args p, hipStream_t st) {
   constexpr int kC = sizeof(T) == 4 ? 32 : 64;
   const LinearAttention& a = p.a;
+  const int64_t all = a.batch * a.v_heads * a.keys * a.values, wgs_all = (all + 255) / 256;
+  const dim3 each((unsigned)(wgs_all < 4096 ? wgs_all : 4096));
+  // over its own initial state a final one goes by way of the workspace
+  const bool apart = a.final_state && a.final_state == a.init && read_elsewhere(p);
+  p.final_state = apart ? a.workspace + (p.spans - 1) * (all + a.batch * a.v_heads) : a.final_state;
   if (p.spans > 1) {
     Args s = p;
     s.groups = (int)(a.v_heads / kHeads);
     attention_kernel<T, kKeys, kTiles, kHeads, kC, false>
         <<<dim3((unsigned)(a.batch * s.groups * p.slices * (p.spans - 1))), 256, 0, st>>>(s);
-    const int64_t states = a.batch * a.v_heads * a.keys * a.values, wgs = (states + 255) / 256;
-    attention_join_kernel<<<dim3((unsigned)(wgs < 4096 ? wgs : 4096)), 256, 0, st>>>(p);
+    attention_join_kernel<<<each, 256, 0, st>>>(p);
   }
   attention_kernel<T, kKeys, kTiles, kHeads, kC, true>
       <<<dim3((unsigned)(a.batch * p.groups * p.slices * p.spans)), 256, 0, st>>>(p);
+  if (apart) attention_copy_kernel<<<each, 256, 0, st>>>(p.final_state, a.final_state, all);
   return hipGetLastError();
 }
 
@@ -973,7 +988,8 @@ template <typename T> hipError_t run_step(const LinearAttention& a, hipStream_t 
 
 int64_t linear_attention_workspace(const LinearAttention& a) {
   const Args p = plan(a);
-  return (p.spans - 1) * a.batch * a.v_heads * (a.keys * a.values + 1);
+  const int64_t states = a.batch * a.v_heads * a.keys * a.values;
+  return (p.spans - 1) * (states + a.batch * a.v_heads) + (read_elsewhere(p) ? states : 0);
 }
 
 hipError_t launch_linear_attention(const LinearAttention& a, hipStream_t st) {

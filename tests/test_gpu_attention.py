@@ -242,6 +242,24 @@ def test_state_in_place_and_streams(ssdi8):
     assert torch.equal(y, want["y"]) and torch.equal(state, want["final_state"])
 
 
+@pytest.mark.parametrize("L,Hq,Hk,Hv", [(2000, 1, 1, 1), (100, 4, 1, 2), (1500, 4, 2, 2), (0, 2, 1, 1)])
+def test_state_in_place(ssdi8, L, Hq, Hk, Hv):
+    """final_state over init_state where several spans, or several heads of y, begin from it."""
+    import ctypes
+    t = draw(L, 2, L, Hq, Hk, Hv, 64, 64, F16)
+    want = ssdi8.linear_attention(t["q"], t["k"], t["v"], t["g"], init_state=t["init"])
+    state = t["init"].clone()
+    d, a, y = ssdi8._attention(t["q"], t["k"], t["v"], t["g"], None, None, None)
+    a.init_state = a.final_state = state.data_ptr()
+    need = ssdi8.linear_attention_workspace_size(d, F16)
+    assert need >= state.numel() * 4
+    ws = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")
+    a.workspace, a.workspace_bytes = ws.data_ptr(), need
+    assert ssdi8.lib().ssdi8_linear_attention(ctypes.byref(d), ctypes.byref(a), torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(y, want["y"]) and torch.equal(state, want["final_state"])
+    assert (ws[need:] == 255).all()
+
+
 def test_captured(ssdi8):
     """Two graphs with eager calls between their replays; each replay equals the eager result."""
     a, b = draw(7, 1, 1100, 2, 2, 2, 64, 64, F16), draw(8, 1, 1300, 1, 1, 2, 64, 64, BF16)

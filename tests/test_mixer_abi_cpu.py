@@ -41,17 +41,25 @@ def test_linear_attention(ssdi8):
         if "seqlen" not in n:
             assert step(a, **n) == s.ERR_SHAPE, n
     assert call(a, keys=257) == step(a, keys=257) == s.ERR_UNSUPPORTED
+    # 64 tokens of 2e9 bytes or more; of one token alone no stride is used
+    ws = dict(workspace=A16, workspace_bytes=1 << 40)
+    for f in ("q_token_stride", "k_token_stride", "v_token_stride"):
+        assert call(changed(a, **{f: 15_624_800}, **ws)) == s.ERR_UNSUPPORTED
+        assert call(changed(a, **{f: 15_624_800}, **ws), batch=0, seqlen=1) == s.OK
+    assert call(changed(a, v_head_stride=15_624_800 * 32, **ws)) == s.ERR_UNSUPPORTED
     assert L.ssdi8_linear_attention(None, ctypes.byref(a), None) == s.ERR_NULL
     assert L.ssdi8_linear_attention(ctypes.byref(s.AttnDims(**sizes)), None, None) == s.ERR_NULL
     assert call(a, batch=0) == step(a, batch=0) == s.OK and size(batch=0) == size(batch=0, seqlen=1 << 20) == 0
     none = changed(a, q=None, k=None, v=None, y=None, final_state=None)
-    assert call(none, seqlen=0) == s.OK and size(seqlen=0) == 0
-    # few heads over many tokens need a workspace: a state and a decay for every span but the last
-    need = size(seqlen=100000)
-    assert need > 0 and need % (4 * 2 * 2 * (64 * 48 + 1)) == 0
+    assert call(none, seqlen=0) == s.OK and size(seqlen=0, q_heads=2) == 0
+    # few heads over many tokens need a workspace: a state and a decay for every span but the last, and the states
+    # once more; heads of y that share a state these alone
+    need, states = size(seqlen=100000), 4 * 2 * 2 * 64 * 48
+    assert need > states and (need - states) % (states + 4 * 2 * 2) == 0 and size(seqlen=100000, q_heads=2) > 0
+    assert size(seqlen=10) == states and size(seqlen=10, q_heads=2) == 0
     assert call(a, seqlen=100000) == s.ERR_WORKSPACE
     assert call(changed(a, workspace=A16, workspace_bytes=need - 1), seqlen=100000) == s.ERR_WORKSPACE
-    assert size(seqlen=1) == 0
+    assert size(seqlen=1, q_heads=2) == 0
     assert L.ssdi8_linear_attention_workspace_size(ctypes.byref(s.AttnDims(**{**sizes, "seqlen": 100000})), s.I8) == 0
     assert L.ssdi8_linear_attention_workspace_size(None, s.F16) == 0
 
