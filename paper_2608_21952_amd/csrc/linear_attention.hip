@@ -784,17 +784,36 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         __builtin_amdgcn_exp2f((float)total);
 }
 
-// The spans' own states into the states behind them: S_s = decay_s S_{s-1} + S_s, from the initial one.
+// The spans' own states into the states behind them: S_s = decay_s S_{s-1} + S_s, from the initial one.  Bound by the
+// latency of the loads where there are many spans: kAtOnce of them are on their way together.
 __global__ __launch_bounds__(256) void attention_join_kernel(Args p) {
   const LinearAttention& a = p.a;
+  constexpr int kAtOnce = 8;
+  const int n = p.spans - 1;
   const int64_t size = state_floats(a), states = a.batch * a.v_heads * size;
   const float* decays = a.workspace + (p.spans - 1) * states;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < states; i += (int64_t)gridDim.x * 256) {
     float s = a.init ? a.init[i] : 0.0f;
-    for (int k = 0; k < p.spans - 1; ++k) {
-      float* at = a.workspace + k * states + i;
-      s = __builtin_fmaf(s, decays[k * a.batch * a.v_heads + i / size], *at);
-      *at = s;
+    const int64_t head = i / size;
+    if (n < kAtOnce) {
+      for (int k = 0; k < n; ++k) {
+        float* at = a.workspace + k * states + i;
+        s = __builtin_fmaf(s, decays[k * a.batch * a.v_heads + head], *at);
+        *at = s;
+      }
+      continue;
+    }
+    for (int k0 = 0; k0 < n; k0 += kAtOnce) {
+      float own[kAtOnce], d[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int k = k0 + u < n ? k0 + u : n - 1;
+        own[u] = a.workspace[k * states + i];
+        d[u] = decays[k * a.batch * a.v_heads + head];
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+        if (k0 + u < n) a.workspace[(k0 + u) * states + i] = s = __builtin_fmaf(s, d[u], own[u]);
     }
   }
 }
@@ -919,17 +938,27 @@ bool paired(const LinearAttention& a) {
   return a.values <= 64 && a.keys <= 128 && a.heads == a.v_heads && a.heads / a.q_heads % 2 == 0 && a.heads / a.k_heads % 2 == 0;
 }
 
+// Columns of a workgroup: 64 where 128 would leave half of the card without work, even with the tokens cut into spans of
+// four chunks: a narrow workgroup is through a chunk sooner.  us with 64 / 128: 1 x 256 tokens, 16 heads of 128 x 128 19 / 26,
+// 4 x 256, 64 heads 31 / 34, 4 x 2000, 8 heads 56 / 63; above, q k is formed twice: 4 x 8192, 16 heads 220 with 128.
+int64_t slice_of(const LinearAttention& a) {
+  if (a.values <= 64 || a.keys > 128) return 64;
+  const int64_t chunks = (a.seqlen + chunk_of(a.dtype) - 1) / chunk_of(a.dtype), spans = chunks < 8 ? 1 : chunks / 4;
+  return a.batch * a.heads * ((a.values + 127) / 128) * spans <= 256 ? 64 : 128;
+}
+
 Args plan(const LinearAttention& a) {
   Args p;
   p.a = a;
-  const int64_t c = chunk_of(a.dtype), slice = a.values <= 64 || a.keys > 128 ? 64 : 128;
+  const int64_t c = chunk_of(a.dtype), slice = slice_of(a);
   p.slices = (int)((a.values + slice - 1) / slice);
   p.chunks = (int)((a.seqlen + c - 1) / c);
   p.groups = (int)(paired(a) ? a.heads / 2 : a.heads);
-  // Spans: as many workgroups as the card holds at once (two for every CU), each with four chunks at least.
-  const int64_t wgs = a.batch * p.groups * p.slices, hold = a.keys > 128 ? 256 : 512;
+  // Spans: as many workgroups as the card holds at once (two for every CU), each with two chunks at least; none of
+  // fewer than eight chunks.  us with and without: 8 chunks of 8 heads of 128 x 128 28 / 37, four chunks of 16 heads 27 / 19.
+  const int64_t wgs = a.batch * p.groups * p.slices, hold = a.keys > 128 ? 256 : 512, most = p.chunks < 8 ? 1 : p.chunks / 2;
   int64_t spans = wgs == 0 ? 1 : hold / wgs;
-  spans = spans < p.chunks / 4 ? spans : p.chunks / 4;
+  spans = spans < most ? spans : most;
   if (spans < 1) spans = 1;
   p.span_chunks = (int)((p.chunks + spans - 1) / spans);
   p.spans = p.span_chunks ? (p.chunks + p.span_chunks - 1) / p.span_chunks : 1;
@@ -964,7 +993,7 @@ template <typename T, int kKeys> hipError_t by_values(const Args& p, hipStream_t
   if constexpr (kKeys > 128) {
     return run<T, kKeys, 1, 1>(p, st);
   } else {
-    if (p.a.values > 64) return run<T, kKeys, 2, 1>(p, st);
+    if (slice_of(p.a) > 64) return run<T, kKeys, 2, 1>(p, st);
     return paired(p.a) ? run<T, kKeys, 2, 2>(p, st) : run<T, kKeys, 1, 1>(p, st);
   }
 }

@@ -66,6 +66,25 @@ def test_lengths(ssdi8, dtype):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("b,L,Hq,Hk,Hv,K,V", [(9, 130, 30, 30, 30, 64, 128), (3, 101, 90, 30, 30, 100, 72),
+                                              (17, 70, 8, 8, 16, 128, 130), (3, 150, 1, 1, 4, 100, 50), (2, 140, 2, 1, 4, 64, 64)])
+def test_many_heads_and_pairs(ssdi8, b, L, Hq, Hk, Hv, K, V, dtype):
+    """Enough heads for workgroups of 128 columns, and heads that share q and k two by two; lengths inside a chunk; one
+    value of v that is no number takes its column from its token on, and no other."""
+    t = draw(L + V, b, L, Hq, Hk, Hv, K, V, dtype)
+    lengths = [L - 13 * i if i < 7 else 1 for i in range(b)]
+    out = check(ssdi8, t, lengths)
+    t["v"][0, 67, 1, V - 1] = float("nan")
+    bad = ssdi8.linear_attention(t["q"], t["k"], t["v"], t["g"], init_state=t["init"],
+                                 lengths=torch.tensor(lengths, dtype=torch.int32).cuda())
+    H, same = max(Hq, Hv), torch.ones_like(out["y"], dtype=torch.bool)
+    for h in range(H):
+        if h * Hv // H == 1:
+            same[0, 67:, h, V - 1] = False
+    assert torch.equal(bad["y"][same], out["y"][same]) and torch.isnan(bad["y"][~same]).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("b,L,H,K,V", [(1, 3000, 2, 64, 64), (2, 1025, 1, 128, 128), (1, 2049, 3, 100, 80)])
 def test_long_sequences_of_few_heads_are_cut(ssdi8, b, L, H, K, V, dtype):
     d = ssdi8.AttnDims(b, L, H, H, H, K, V)
