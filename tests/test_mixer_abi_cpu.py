@@ -46,7 +46,9 @@ def test_linear_attention(ssdi8):
     for f in ("q_token_stride", "k_token_stride", "v_token_stride"):
         assert call(changed(a, **{f: 15_624_800}, **ws)) == s.ERR_UNSUPPORTED
         assert call(changed(a, **{f: 15_624_800}, **ws), batch=0, seqlen=1) == s.OK
-    assert call(changed(a, v_head_stride=15_624_800 * 32, **ws)) == s.ERR_UNSUPPORTED
+    far = changed(a, v_head_stride=15_624_800 * 32, **ws)   # heads are taken two by two, of one token too
+    assert call(far) == call(far, seqlen=1) == s.ERR_UNSUPPORTED
+    assert call(far, batch=0, v_heads=1) == s.OK
     assert L.ssdi8_linear_attention(None, ctypes.byref(a), None) == s.ERR_NULL
     assert L.ssdi8_linear_attention(ctypes.byref(s.AttnDims(**sizes)), None, None) == s.ERR_NULL
     assert call(a, batch=0) == step(a, batch=0) == s.OK and size(batch=0) == size(batch=0, seqlen=1 << 20) == 0
