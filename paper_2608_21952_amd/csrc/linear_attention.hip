@@ -23,8 +23,9 @@
 //
 // What bounds it: of a chunk's 9 us with two workgroups on a CU the products take 2; the rest is LDS reads of the
 // operands, S's conversion for every chunk, and the barriers between the phases.  Two heads that share q and k read them once.
-// 4 x 4096 tokens, 80 heads of 64 with shared q and k of 128, fp16: 195 us, with the spans' states 87 and their join 12
-// beside them (1.5 TB/s in all); 4 x 8192, 16 heads of 128 x 128, bf16: 2.4 TB/s; 16384 of 8 heads of 64 x 128, fp32: 79 + 40 + 11.
+// 4 x 4096 tokens, 80 heads of 64 with shared q and k of 128, fp16: 179 us, with the spans' states 80 and their join 13
+// beside them (1.5 TB/s in all); 4 x 8192, 16 heads of 128 x 128, bf16: 156 + 83 + 13; 16384 of 8 heads of 64 x 128, fp32:
+// 77 + 39 + 10.
 #include <type_traits>
 
 #include "attention.hpp"
