@@ -14,9 +14,11 @@
 //
 // Roundings, of 16-bit types: p and S are rounded once on their way into the products for y, which adds to y's error
 // about as much as its own rounding (0.00029 against 0.00021 of y, fp16): as two values each the same walk took 343 us
-// instead of 220.  exp(c_C - c_j) v_j, which would leave its rounding in S with every chunk, enters as the sum of
-// values of the type that leave nothing of fp32's accuracy: two of fp16 (2^-23 off), three of bf16 (two would be
-// 2^-17 off).  fp16: brought to the type's range by powers of two first (p per row, S and v per column).
+// instead of 220.  exp(c_C - c_j) v_j, which would leave its rounding in S with every chunk, enters as the sum of three
+// bf16 values (two would be 2^-17 off), for fp16 too: two fp16 values, brought into range by a power of two per column,
+// lost what decays within a chunk had made small, though a key that is 0 for the later tokens has nothing else.  k of
+// fp16 enters as two bf16 values then: five products where two fp16 values take two, 314 us instead of 246 for 4 x 4096
+// tokens of 80 heads.  fp16: p per row and S per column are brought to the type's range by powers of two.
 // Sums, S, and the decays' sums (these in fp64: differences of far sums) are not rounded.
 // A value of v that is no number would reach earlier tokens of its chunk through 0 times it: it enters as 0, and its
 // column is NaN from its token on.
@@ -27,6 +29,7 @@
 // beside them (1.5 TB/s in all); 4 x 8192, 16 heads of 128 x 128, bf16: 156 + 83 + 13; 16384 of 8 heads of 64 x 128, fp32:
 // 77 + 39 + 10.
 #include <type_traits>
+#include <utility>
 
 #include "attention.hpp"
 #include "block.hpp"
@@ -151,6 +154,23 @@ template <typename T, typename At> __device__ __forceinline__ Frag<T> column_fra
   return f;
 }
 
+// Eight fp16 values as two bf16 each, which hold their 11 bits.
+__device__ __forceinline__ void split_halves(const Frag<_Float16>& k, bf16* hi, bf16* lo) {
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = (float)k.v[e];
+  const Frag<bf16> h = round_frag<bf16>(f);
+  take_off(f, h);
+  const Frag<bf16> l = round_frag<bf16>(f);
+  __builtin_memcpy(__builtin_assume_aligned(hi, 16), &h, 16);
+  __builtin_memcpy(__builtin_assume_aligned(lo, 16), &l, 16);
+}
+
+// f(0), f(1) and so on, the numbers as types.
+template <int... i, typename F> __device__ __forceinline__ void each_of(std::integer_sequence<int, i...>, F f) {
+  (f(std::integral_constant<int, i>()), ...);
+}
+
 // A condition whose code is to lie out of the way.
 __device__ __forceinline__ bool rarely(bool v) { return __builtin_expect(v, 0); }
 
@@ -225,6 +245,14 @@ template <typename T, int kRows, int kWidth, int kPart> struct Stage {
     for (int i = 0; i < kEach; ++i)
       *reinterpret_cast<uint4*>(lds + at(i * kStep + tid / kVecs, column(tid))) = v[i];
   }
+  // fp16: each value as two of bf16 that add up to it, at the same places of hi and lo.
+  template <typename At> __device__ __forceinline__ void put_halves(bf16* hi, bf16* lo, int tid, At at) const {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int o = at(i * kStep + tid / kVecs, column(tid));
+      split_halves(__builtin_bit_cast(Frag<_Float16>, v[i]), hi + o, lo + o);
+    }
+  }
 };
 
 // The magnitude bits of a fragment's largest value (as those of the type), 16-bit types.
@@ -271,7 +299,12 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
   constexpr int kOutSize = kC * kSlice * kHeads;             // of y's tile, which takes the place of q
   __shared__ __attribute__((aligned(16))) T q_lds[kOut ? (kC * kKeys > kOutSize ? kC * kKeys : kOutSize) : 8];
   __shared__ __attribute__((aligned(16))) T k_lds[kC * kKeys];
-  __shared__ __attribute__((aligned(16))) T v_lds[kC * kV];
+  // k as bf16 (fp16): with outputs its first values take its own place when p is there, the second ones that of v,
+  // which all waves have in registers then
+  constexpr int kVSize = kF16 && kOut && kC * kKeys > kC * kV ? kC * kKeys : kC * kV;
+  __shared__ __attribute__((aligned(16))) T v_lds[kVSize];
+  __shared__ __attribute__((aligned(16))) T rest_lds[kF16 && !kOut ? kC * kKeys : 8];
+  bf16 *k_hi = reinterpret_cast<bf16*>(k_lds), *k_lo = reinterpret_cast<bf16*>(kOut ? v_lds : rest_lds);
   __shared__ __attribute__((aligned(16))) Frag<T> p_lds[kHeads][kOut ? kPairs * 64 : 1];
   __shared__ __attribute__((aligned(16))) double c_all[kHeads][kC];
   __shared__ __attribute__((aligned(16))) float w_all[kHeads][kC], e_all[kHeads][kC], row_all[kHeads][kC];
@@ -392,7 +425,8 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
     const int lane = g * 16 + m;
     __syncthreads();   // the last chunk is read
     if constexpr (kOut) q_next.put(q_lds, tid, k_at);
-    k_next.put(k_lds, tid, k_at);
+    if constexpr (kF16 && !kOut) k_next.put_halves(k_hi, k_lo, tid, k_at);
+    else k_next.put(k_lds, tid, k_at);
     v_next.put(v_lds, tid, v_at);
     // sums of the decays' logarithms, in base 2; below 2^-65536 is 0 all the same, and an infinite one would leave
     // no differences behind it
@@ -409,25 +443,20 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
     const int64_t t0 = (int64_t)chunk * kC;
     // v, 0 where its values are no numbers
     Frag<T> vf[kSums][kTiles];
-    uint32_t most_v[kTiles];
     int first[kTiles];   // the first token of the column whose value is no number
     constexpr uint32_t kNoNumber = kF16 ? 0x7c00u : kHalf ? 0x7f80u : 0x7f800000u;
-    auto largest_v = [&](int n) {
-      uint32_t big = 0;
-#pragma unroll
-      for (int s = 0; s < kSums; ++s) big = largest(vf[s][n], big);
-      return !kHalf ? big : (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16;
-    };
     bool odd = false;
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
       first[n] = kC;
+      uint32_t big = 0;
 #pragma unroll
-      for (int s = 0; s < kSums; ++s)
+      for (int s = 0; s < kSums; ++s) {
         vf[s][n] = column_frag(v_lds + 32 * s * kV + sub * kSlice + my0 + 16 * n, lane,
                                [&](int row, int c) { return v_at(row, 4 * c); });
-      most_v[n] = largest_v(n);
-      odd |= most_v[n] >= kNoNumber;
+        big = largest(vf[s][n], big);
+      }
+      odd |= (!kHalf ? big : (big & 0xffffu) > (big >> 16) ? big & 0xffffu : big >> 16) >= kNoNumber;
     }
     const bool any_bad = __any(odd) != 0;
     if (rarely(any_bad)) {
@@ -442,7 +471,6 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
               first[n] = j < first[n] ? j : first[n];
               vf[s][n].v[e] = (T)0.0f;
             }
-        most_v[n] = largest_v(n);
 #pragma unroll
         for (int d = 16; d < 64; d *= 2) {
           const int o = __shfl_xor(first[n], d);
@@ -565,6 +593,8 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         __builtin_amdgcn_sched_barrier(0);
       }
       __syncthreads();   // p is there
+      if constexpr (kF16) k_next.put_halves(k_hi, k_lo, tid, k_at);
+      __builtin_amdgcn_sched_barrier(0);
     }
 
     if constexpr (kOut) {
@@ -677,43 +707,46 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
       }
     }
     __builtin_amdgcn_sched_barrier(0);
-    // The state behind the chunk: v times exp(c_end - c_j), as kTerms values of the type
-    constexpr int kTerms = kF16 ? 2 : kHalf ? 3 : 1;
+    // The state behind the chunk: v times exp(c_end - c_j) as kTerms values, of 16-bit types of bf16, whose range is
+    // fp32's: decays within a chunk span more than fp16's, and where k or v of the later tokens is 0 what is left of the
+    // earlier ones is all there is.  k of fp16 enters as two of bf16, which hold its 11 bits.
+    typedef std::conditional_t<kHalf, bf16, float> Term;
+    constexpr int kTerms = kHalf ? 3 : 1;
     const float decay = __builtin_amdgcn_exp2f((float)c_end);
-    int v_shift[kTiles];
 #pragma unroll
     for (int n = 0; n < kTiles; ++n) {
-      v_shift[n] = 0;
-      if constexpr (kF16) {
-        // as fp32's bits; the decays only make the values smaller
-        const float most = (float)__builtin_bit_cast(_Float16, (uint16_t)group_max(most_v[n]));
-        v_shift[n] = range_shift<-2>(__builtin_bit_cast(uint32_t, most));
-      }
       // a column with a value that is no number is NaN from here on
-      const float by = first[n] < kC ? __builtin_nanf("") : kF16 ? decay * power(v_shift[n]) : decay;
+      const float by = first[n] < kC ? __builtin_nanf("") : decay;
 #pragma unroll
       for (int t = 0; t < kKeyT; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) S[t][n][r] *= by;
     }
-    // k's columns are read four key tiles ahead: each read at its use, the products waited for it 16 times (4000 to
+    if constexpr (kF16 && kOut) __syncthreads();   // k's halves are there
+    // k's columns are read several key tiles ahead: each read at its use, the products waited for it 16 times (4000 to
     // 5700 cycles for 1024 of products).
-    constexpr int kAhead = kKeyT < 4 ? kKeyT : 4, kParts = kSums * kKeyT / kAhead;
-    Frag<T> kf[2][kAhead];
-    auto read_k = [&](int part) {
+    constexpr int kAhead = kF16 ? 2 : kKeyT < 4 ? kKeyT : 4, kParts = kSums * kKeyT / kAhead;
+    Frag<Term> kf[2][kAhead], kr[2][kF16 ? kAhead : 1];
+    auto read_k = [&](auto part_) {
+      constexpr int part = decltype(part_)::value, s = part * kAhead / kKeyT;
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const int s = part * kAhead / kKeyT, t = part * kAhead % kKeyT + u;
-        kf[part % 2][u] = column_frag(k_lds + 32 * s * kKeys, lane, [&](int row, int c) { return k_at(row, key_of(t, c)); });
+        const int t = part * kAhead % kKeyT + u;
+        auto at = [&](int row, int c) { return k_at(row, key_of(t, c)); };
+        if constexpr (kF16) {
+          kf[part % 2][u] = column_frag(k_hi + 32 * s * kKeys, lane, at);
+          kr[part % 2][u] = column_frag(k_lo + 32 * s * kKeys, lane, at);
+        } else {
+          kf[part % 2][u] = column_frag(k_lds + 32 * s * kKeys, lane, at);
+        }
       }
     };
-    read_k(0);
-    Frag<T> w_v[kTerms][kTiles];
-#pragma unroll
-    for (int part = 0; part < kParts; ++part) {
-      const int s = part * kAhead / kKeyT, t0 = part * kAhead % kKeyT;
-      if (part + 1 < kParts) read_k(part + 1);
-      if (t0 == 0) {
+    read_k(std::integral_constant<int, 0>());
+    Frag<Term> w_v[kTerms][kTiles];
+    each_of(std::make_integer_sequence<int, kParts>(), [&](auto part_) {
+      constexpr int part = decltype(part_)::value, s = part * kAhead / kKeyT, t0 = part * kAhead % kKeyT;
+      if constexpr (part + 1 < kParts) read_k(std::integral_constant<int, part + 1>());
+      if constexpr (t0 == 0) {
         const float4 wa = *reinterpret_cast<const float4*>(w_lds + 32 * s + 4 * g);
         const float4 wb = *reinterpret_cast<const float4*>(w_lds + 32 * s + 16 + 4 * g);
         const float w[8] = {wa.x, wa.y, wa.z, wa.w, wb.x, wb.y, wb.z, wb.w};
@@ -721,10 +754,10 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
         for (int n = 0; n < kTiles; ++n) {
           float f[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * (kF16 ? w[e] * power(v_shift[n]) : w[e]);
+          for (int e = 0; e < 8; ++e) f[e] = (float)vf[s][n].v[e] * w[e];
 #pragma unroll
           for (int i = 0; i < kTerms; ++i) {
-            w_v[i][n] = round_frag<T>(f);
+            w_v[i][n] = round_frag<Term>(f);
             if (i + 1 < kTerms) take_off(f, w_v[i][n]);
           }
         }
@@ -738,23 +771,23 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int u = 0; u < kAhead; ++u) {
-        const Frag<T>& k = kf[part % 2][u];
         const int t = t0 + u;
+        auto products = [&](const Frag<Term>& k, auto terms) {
 #pragma unroll
-        for (int i = 0; i < kTerms; ++i)
+          for (int i = 0; i < decltype(terms)::value; ++i)
 #pragma unroll
-          for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, w_v[i][n], S[t][n]);
+            for (int n = 0; n < kTiles; ++n) S[t][n] = mma(k, w_v[i][n], S[t][n]);
+        };
+        products(kf[part % 2][u], std::integral_constant<int, kTerms>());
+        // the third term's product with k's second value is below 2^-25
+        if constexpr (kF16) products(kr[part % 2][u], std::integral_constant<int, 2>());
       }
+      // Behind a branch, as the next loads have them, the compiler leaves out wait states that a register written by a
+      // product, or overwritten after one, needs: eight of them here.
       __builtin_amdgcn_sched_barrier(0);
-    }
-    if constexpr (kF16) {   // without a branch, which would have S in the registers twice
-#pragma unroll
-      for (int n = 0; n < kTiles; ++n)
-#pragma unroll
-        for (int t = 0; t < kKeyT; ++t)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) S[t][n][r] *= power(-v_shift[n]);
-    }
+      asm volatile("s_nop 7");
+      __builtin_amdgcn_sched_barrier(0);
+    });
     total += c_end;
   }
 
