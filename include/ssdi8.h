@@ -498,11 +498,13 @@ ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_
  * 1 <= keys <= 256, values >= 1, any seqlen.  q, k and v lie at strides (batch, token, head), a head's values dense.
  * init_state and final_state may be the same memory.  With seqlen = 0 q, k, v and y may be NULL.
  * Values that are no numbers: of v, its column of y and of the state are NaN from its token on; of q, k and
- * g, what the formula gives; earlier tokens are not touched.  A decay of exp(-65536) or less is 0.
+ * g, what the formula gives, where an infinity of the formula may be a NaN; earlier tokens are not touched.  A decay of exp(-65536) or less is 0.
  * The workspace holds the states of the spans that long sequences of few heads are cut into, and final states on
  * their way over init_state where several workgroups read that.
- * 16-bit types: products of rounded operands, so y is off by about its own rounding once more; the state keeps fp32's
- * accuracy.  64 neighbouring tokens of q, k, v and y span less than 2e9 bytes each, and so do
+ * 16-bit types: products of rounded operands, so y is off by about its own rounding once more, relative to the sum of its
+ * terms' magnitudes; of fp16 a term's weight (of 64 tokens) or element of the state that is below 2^-28 of the largest one
+ * of its row, or column, is off by up to 2^-39 of that.  The state keeps fp32's accuracy: every element, relative to the
+ * magnitudes of its own terms.  64 neighbouring tokens of q, k, v and y span less than 2e9 bytes each, and so do
  * two heads of v (SSDI8_ERR_UNSUPPORTED).
  */
 typedef struct {

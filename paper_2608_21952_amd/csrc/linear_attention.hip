@@ -88,15 +88,14 @@ template <typename T> __device__ __forceinline__ void take_off(float (&f)[8], co
   for (int e = 0; e < 8; ++e) f[e] -= (float)hi.v[e];
 }
 
-// fp16: the exponent shift that brings values of which the largest has magnitude bits `big` (fp32) to where they
-// round well: none for a largest one in [2^kLow, 2^15), else to [2^14, 2^15); none for 0 and for what is no number.
-// Below the normal range values are off by 2^-25: of a sum over 64 of them with a largest one of 2^-6 at most 2^-13,
-// less than their own rounding.
-template <int kLow> __device__ __forceinline__ int range_shift(uint32_t big) {
+// fp16: the exponent shift that brings values of which the largest has magnitude bits `big` (fp32) to where that lies in
+// [2^14, 2^15), at most kMost; none for 0 and for what is no number.  Below fp16's normal range values are off by 2^-25:
+// by 2^-39 of the largest, as long as that is 2^(14 - kMost) or more.
+template <int kMost> __device__ __forceinline__ int range_shift(uint32_t big) {
   const int e = (int)(big >> 23);
-  if (e == 0 || e == 255 || (e >= 127 + kLow && e < 127 + 15)) return 0;
+  if (e == 0 || e == 255) return 0;
   const int s = 127 + 14 - e;
-  return s > 100 ? 100 : s;
+  return s > kMost ? kMost : s;
 }
 __device__ __forceinline__ float power(int e) { return __builtin_bit_cast(float, (uint32_t)(e + 127) << 23); }
 __device__ __forceinline__ uint32_t bits_max(uint32_t a, float v) {
@@ -529,14 +528,13 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           for (int r = 0; r < 4; ++r) big = __builtin_fmaxf(big, __builtin_fabsf(acc[jt][r]));
         }
         if constexpr (kF16) {
-          const int sh = range_shift<-6>(group_max(__builtin_bit_cast(uint32_t, big)));
-          if (g == 0) row_scale[i] = power(sh);
-          if (rarely(__any(sh != 0))) {
+          // p below 2^-48 times 64 values is nothing to y; a row's sums stay finite where y is below 2^65
+          const float by = power(range_shift<62>(group_max(__builtin_bit_cast(uint32_t, big))));
+          if (g == 0) row_scale[i] = by;
 #pragma unroll
-            for (int jt = 0; jt < kRowsT; ++jt)
+          for (int jt = 0; jt < kRowsT; ++jt)
 #pragma unroll
-              for (int r = 0; r < 4; ++r) acc[jt][r] *= power(sh);
-          }
+            for (int r = 0; r < 4; ++r) acc[jt][r] *= by;
         }
         const int pair0 = it / 2 * (it / 2 + 1) + it % 2 * (it / 2 + 1);
 #pragma unroll
@@ -552,7 +550,6 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
 
     v4f acc[kOut ? kRowsT : 1][kTiles] = {};
     int s_shift[kTiles];        // of the lane's column of the state
-    bool any_shift = false;
     if constexpr (kOut) {
       // S^T q, the state rounded to the type
       __builtin_amdgcn_sched_barrier(0);   // phases stay apart: their operands do not fit the registers together
@@ -565,8 +562,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           for (int t = 0; t < kKeyT; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) most = __builtin_fmaxf(most, __builtin_fabsf(S[t][n][r]));
-          s_shift[n] = range_shift<-6>(group_max(__builtin_bit_cast(uint32_t, most)));
-          any_shift |= __any(s_shift[n] != 0) != 0;
+          s_shift[n] = range_shift<100>(group_max(__builtin_bit_cast(uint32_t, most)));
         }
       }
       Frag<T> qf[2][kRowsT];   // read a step ahead
@@ -609,7 +605,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
           for (int r = 0; r < 4; ++r) acc[it][n][r] *= e;
         }
       }
-      if (rarely(any_shift)) {
+      if constexpr (kF16) {
 #pragma unroll
         for (int n = 0; n < kTiles; ++n)
 #pragma unroll
