@@ -91,6 +91,17 @@ template <int kLanes> __device__ __forceinline__ float lane_sum(float v) {
 }
 
 // ---------------------------------------------------------------------------- launches
+// A launch has fewer than 2^32 threads: more workgroups are given to several, f(first, count) each of them.
+template <typename F> hipError_t in_parts(int64_t workgroups, int threads, F f) {
+  const int64_t most = ((int64_t)1 << 31) / threads;
+  for (int64_t first = 0; first < workgroups; first += most) {
+    f(first, dim3((unsigned)(workgroups - first < most ? workgroups - first : most)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // Element offsets between batch elements and tokens of a [b, l, d] tensor whose d is dense.
 struct Rows {
   int64_t batch = 0, token = 0;

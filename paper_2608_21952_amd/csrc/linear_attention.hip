@@ -178,6 +178,7 @@ struct Args {
   int slices, spans, chunks, span_chunks;   // column slices of a head; spans of the tokens and their chunks
   int groups;                               // of heads: those that a workgroup takes together
   float* final_state;
+  int64_t first;                            // of the launch's workgroups
 };
 
 __device__ __host__ __forceinline__ int64_t state_floats(const LinearAttention& a) { return a.keys * a.values; }
@@ -314,7 +315,7 @@ __global__ __launch_bounds__(256, kKeys > 128 ? 1 : 2) void attention_kernel(Arg
   const int sub = kHeads > 1 ? wave / kWH : 0, hw = wave % kWH;   // head of the workgroup, wave of the head
   double* c_lds = c_all[sub];
   float *w_lds = w_all[sub], *e_lds = e_all[sub], *row_scale = row_all[sub], *b_lds = b_all[sub][hw];
-  int id = xcd_remap(blockIdx.x, gridDim.x);
+  int id = (int)p.first + xcd_remap(blockIdx.x, gridDim.x);
   const int slice = id % p.slices;
   id /= p.slices;
   // heads are neighbours: those that share q and k share an XCD's cache
@@ -872,13 +873,14 @@ __device__ __forceinline__ void store4(float* p, float4 f) {
 // threads.  Bound by the state's bytes: all of a thread's loads are on their way before the first is used.  128 x 80 heads
 // of 128 x 64: 119 us, 5.7 TB/s (154 through the caches).
 template <typename T, int kRows>
-__global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, int slices) {
+__global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, int slices, int64_t first) {
   constexpr int kMost = kRows * 16;
   __shared__ float k_lds[kMost], q_lds[kMost];
   __shared__ float sums[4][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int slice = (int)(blockIdx.x % slices);
-  const int64_t head = blockIdx.x / slices, b = head / a.v_heads;
+  const int64_t id = first + blockIdx.x;
+  const int slice = (int)(id % slices);
+  const int64_t head = id / slices, b = head / a.v_heads;
   const int hv = (int)(head % a.v_heads), keys = (int)a.keys;
   const int hk = (int)(hv * a.k_heads / a.v_heads);
   const int col = slice * 64 + tid % 16 * 4, kr = tid / 16;
@@ -986,6 +988,7 @@ int64_t slice_of(const LinearAttention& a) {
 Args plan(const LinearAttention& a) {
   Args p;
   p.a = a;
+  p.first = 0;
   const int64_t c = chunk_of(a.dtype), slice = slice_of(a);
   p.slices = (int)((a.values + slice - 1) / slice);
   p.chunks = (int)((a.seqlen + c - 1) / c);
@@ -1012,15 +1015,22 @@ template <typename T, int kKeys, int kTiles, int kHeads> hipError_t run(Args p, 
   // over its own initial state a final one goes by way of the workspace
   const bool apart = a.final_state && a.final_state == a.init && read_elsewhere(p);
   p.final_state = apart ? a.workspace + (p.spans - 1) * (all + a.batch * a.v_heads) : a.final_state;
+  auto walk = [&](auto out, Args s, int64_t spans) {
+    return in_parts(a.batch * s.groups * s.slices * spans, 256, [&](int64_t first, dim3 grid) {
+      s.first = first;
+      attention_kernel<T, kKeys, kTiles, kHeads, kC, decltype(out)::value><<<grid, 256, 0, st>>>(s);
+    });
+  };
+  hipError_t e = hipSuccess;
   if (p.spans > 1) {
     Args s = p;
     s.groups = (int)(a.v_heads / kHeads);
-    attention_kernel<T, kKeys, kTiles, kHeads, kC, false>
-        <<<dim3((unsigned)(a.batch * s.groups * p.slices * (p.spans - 1))), 256, 0, st>>>(s);
+    e = walk(std::false_type(), s, p.spans - 1);
+    if (e != hipSuccess) return e;
     attention_join_kernel<<<each, 256, 0, st>>>(p);
   }
-  attention_kernel<T, kKeys, kTiles, kHeads, kC, true>
-      <<<dim3((unsigned)(a.batch * p.groups * p.slices * p.spans)), 256, 0, st>>>(p);
+  e = walk(std::true_type(), p, p.spans);
+  if (e != hipSuccess) return e;
   if (apart) attention_copy_kernel<<<each, 256, 0, st>>>(p.final_state, a.final_state, all);
   return hipGetLastError();
 }
@@ -1042,11 +1052,11 @@ template <typename T> hipError_t by_size(const Args& p, hipStream_t st) {
 
 template <typename T> hipError_t run_step(const LinearAttention& a, hipStream_t st) {
   const int slices = (int)((a.values + 63) / 64);
-  const dim3 grid((unsigned)(a.batch * a.v_heads * slices));
-  if (a.keys <= 64) attention_step_kernel<T, 4><<<grid, 256, 0, st>>>(a, slices);
-  else if (a.keys <= 128) attention_step_kernel<T, 8><<<grid, 256, 0, st>>>(a, slices);
-  else attention_step_kernel<T, 16><<<grid, 256, 0, st>>>(a, slices);
-  return hipGetLastError();
+  return in_parts(a.batch * a.v_heads * slices, 256, [&](int64_t first, dim3 grid) {
+    if (a.keys <= 64) attention_step_kernel<T, 4><<<grid, 256, 0, st>>>(a, slices, first);
+    else if (a.keys <= 128) attention_step_kernel<T, 8><<<grid, 256, 0, st>>>(a, slices, first);
+    else attention_step_kernel<T, 16><<<grid, 256, 0, st>>>(a, slices, first);
+  });
 }
 
 }  // namespace

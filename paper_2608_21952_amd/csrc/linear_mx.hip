@@ -85,7 +85,7 @@ __device__ __forceinline__ int slot_key(int r) { return (r >> 1) & 7; }
 
 // kWM x kWN waves, each a (kBM / kWM) x (kBN / kWN) part of the tile.
 template <int kX, int kBM, int kBN, int kWM, int kWN>
-__global__ __launch_bounds__(64 * kWM * kWN) void mx_tile(LinearMx a, int mtiles, int ntiles) {
+__global__ __launch_bounds__(64 * kWM * kWN) void mx_tile(LinearMx a, int mtiles, int ntiles, int first) {
   constexpr int kThreads = 64 * kWM * kWN;
   constexpr int kXL = kX == kE4m3 ? 2 : 1;   // lines of a row of x per k-tile
   constexpr int kTM = kBM / kWM / 32, kTN = kBN / kWN / 32;
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(64 * kWM * kWN) void mx_tile(LinearMx a, int mtiles
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave / kWN, wn = wave % kWN;
   // tiles of one XCD lie together: bands of four rows of tiles, column by column
-  const int id = xcd_remap(blockIdx.x, mtiles * ntiles);
+  const int id = first + xcd_remap(blockIdx.x, gridDim.x);
   constexpr int kBand = 4;
   const int band = id / (kBand * ntiles), in = id % (kBand * ntiles);
   const int rows = mtiles - band * kBand < kBand ? mtiles - band * kBand : kBand;
@@ -303,11 +303,11 @@ __global__ __launch_bounds__(64 * kWM * kWN) void mx_tile(LinearMx a, int mtiles
 
 // 16 rows of w by kMT x 16 rows of x per workgroup of kWaves waves.
 template <int kX, int kMT, int kWaves>
-__global__ __launch_bounds__(64 * kWaves) void mx_rows(LinearMx a) {
+__global__ __launch_bounds__(64 * kWaves) void mx_rows(LinearMx a, int64_t first) {
   constexpr int kXL = kX == kE4m3 ? 2 : 1;
   __shared__ float part[kWaves][kMT][256];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t n0 = (first + blockIdx.x) * 16;
   const int lines = (int)((a.blocks + kTileBlocks - 1) / kTileBlocks);
   const int fr = lane & 15, fg = lane >> 4;
   const int64_t n = n0 + fr < a.n ? n0 + fr : a.n - 1;
@@ -395,8 +395,9 @@ __global__ __launch_bounds__(64 * kWaves) void mx_rows(LinearMx a) {
 
 template <int kX, int kBM, int kBN, int kWM, int kWN> hipError_t run_tile(const LinearMx& a, hipStream_t st) {
   const int64_t mt = (a.m + kBM - 1) / kBM, nt = (a.n + kBN - 1) / kBN;
-  mx_tile<kX, kBM, kBN, kWM, kWN><<<dim3((unsigned)(mt * nt)), 64 * kWM * kWN, 0, st>>>(a, (int)mt, (int)nt);
-  return hipGetLastError();
+  return in_parts(mt * nt, 64 * kWM * kWN, [&](int64_t first, dim3 grid) {
+    mx_tile<kX, kBM, kBN, kWM, kWN><<<grid, 64 * kWM * kWN, 0, st>>>(a, (int)mt, (int)nt, (int)first);
+  });
 }
 
 template <int kX> hipError_t by_tiles(const LinearMx& a, hipStream_t st) {
@@ -416,11 +417,11 @@ template <int kX> hipError_t by_tiles(const LinearMx& a, hipStream_t st) {
 }
 
 template <int kX> hipError_t run(const LinearMx& a, hipStream_t st) {
-  const unsigned strips = (unsigned)((a.n + 15) / 16);
-  if (a.m <= 16) mx_rows<kX, 1, 8><<<strips, 512, 0, st>>>(a);
-  else if (a.m <= 32) mx_rows<kX, 2, 8><<<strips, 512, 0, st>>>(a);
-  else return by_tiles<kX>(a, st);
-  return hipGetLastError();
+  if (a.m > 32) return by_tiles<kX>(a, st);
+  return in_parts((a.n + 15) / 16, 512, [&](int64_t first, dim3 grid) {
+    if (a.m <= 16) mx_rows<kX, 1, 8><<<grid, 512, 0, st>>>(a, first);
+    else mx_rows<kX, 2, 8><<<grid, 512, 0, st>>>(a, first);
+  });
 }
 
 }  // namespace

@@ -75,13 +75,13 @@ __device__ __forceinline__ uint32_t biggest_of(const float (&v)[kVec], uint32_t 
 
 // kGroups: several groups of a width that is a multiple of eight.  kMost vectors of every thread, all whole.
 template <typename T, bool kWave, int kMost, int kThreads, bool kGroups, bool kZ, bool kR>
-__global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int walk) {
+__global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int walk, int64_t first) {
   extern __shared__ float terms_all[];
   __shared__ float part[2][16];
   __shared__ uint32_t biggest[2][16];
   const int t = kWave ? threadIdx.x & 63 : threadIdx.x;
   const int threads = kWave ? 64 : blockDim.x;
-  const int64_t item = kWave ? (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6) : blockIdx.x;
+  const int64_t item = kWave ? (first + blockIdx.x) * 4 + (threadIdx.x >> 6) : first + blockIdx.x;
   const int64_t row0 = item * walk;
   if (row0 >= a.rows) return;   // whole waves, and none where a barrier follows
   const int64_t row1 = row0 + walk < a.rows ? row0 + walk : a.rows;
@@ -243,12 +243,12 @@ __global__ __launch_bounds__(kThreads) void norm_quantize_kernel(Args a, int wal
 }
 
 // A row's values in LDS, a workgroup for each row.
-template <typename T> __global__ __launch_bounds__(1024) void norm_quantize_lds_kernel(Args a) {
+template <typename T> __global__ __launch_bounds__(1024) void norm_quantize_lds_kernel(Args a, int64_t first) {
   extern __shared__ float values[];
   __shared__ float part[16];
   __shared__ uint32_t biggest[16];
   const int t = threadIdx.x, threads = blockDim.x, waves = threads / 64;
-  const int64_t row = blockIdx.x;
+  const int64_t row = first + blockIdx.x;
   const int ends = a.blocks * kMxBlock;   // whole blocks
   auto load = [&](const void* p, int64_t off, int n, float (&v)[kVec]) {
     load_vec<T>(static_cast<const T*>(p) + off, n, v);
@@ -353,8 +353,9 @@ template <typename T> hipError_t run(const Args& a, hipStream_t st) {
                                                hipFuncAttributeMaxDynamicSharedMemorySize, 32768 * 4);
       if (e != hipSuccess) return e;
     }
-    norm_quantize_lds_kernel<T><<<dim3((unsigned)a.rows), threads, lds, st>>>(a);
-    return hipGetLastError();
+    return in_parts(a.rows, threads, [&](int64_t first, dim3 grid) {
+      norm_quantize_lds_kernel<T><<<grid, threads, lds, st>>>(a, first);
+    });
   }
   auto launch = [&](auto wave, auto most, auto limit, auto groups, int threads) {
     constexpr bool kWave = decltype(wave)::value, kGroups = decltype(groups)::value;
@@ -366,10 +367,10 @@ template <typename T> hipError_t run(const Args& a, hipStream_t st) {
     const int64_t count = (a.rows + walk - 1) / walk;
     const size_t lds = kGroups ? sizeof(float) * kItems * (a.D / kVec) : 0;
     auto go = [&](auto z, auto r) {
-      norm_quantize_kernel<T, kWave, decltype(most)::value, decltype(limit)::value, kGroups, decltype(z)::value,
-                           decltype(r)::value>
-          <<<dim3((unsigned)((count + kItems - 1) / kItems)), threads, lds, st>>>(a, walk);
-      return hipGetLastError();
+      return in_parts((count + kItems - 1) / kItems, threads, [&](int64_t first, dim3 grid) {
+        norm_quantize_kernel<T, kWave, decltype(most)::value, decltype(limit)::value, kGroups, decltype(z)::value,
+                             decltype(r)::value><<<grid, threads, lds, st>>>(a, walk, first);
+      });
     };
     if (a.residual) return a.z ? go(std::true_type(), std::true_type()) : go(std::false_type(), std::true_type());
     return a.z ? go(std::true_type(), std::false_type()) : go(std::false_type(), std::false_type());

@@ -12,10 +12,10 @@ constexpr int kUnroll = 4;
 
 template <typename T, int kFormat>
 __global__ __launch_bounds__(256) void quantize_mx_kernel(const T* x, int64_t x_row, int64_t rows, int k,
-                                                          int row_vecs, uint8_t* codes, uint8_t* scales) {
+                                                          int row_vecs, uint8_t* codes, uint8_t* scales, int64_t from) {
   constexpr int kBytes = kFormat == SSDI8_FMT_MXFP8 ? kVec : kVec / 2;
   const int64_t total = rows * row_vecs;
-  const int64_t first = (int64_t)blockIdx.x * (256 * kUnroll) + threadIdx.x;
+  const int64_t first = (from + blockIdx.x) * (256 * kUnroll) + threadIdx.x;
   float v[kUnroll][kVec];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
@@ -37,13 +37,14 @@ __global__ __launch_bounds__(256) void quantize_mx_kernel(const T* x, int64_t x_
 hipError_t launch_quantize_mx(int dtype, int format, int64_t rows, int64_t k, const void* x, int64_t x_row,
                               void* codes, void* scales, hipStream_t st) {
   const int row_vecs = (int)(mx_blocks(k) * (kMxBlock / kVec));
-  const unsigned grid = (unsigned)((rows * row_vecs + 256 * kUnroll - 1) / (256 * kUnroll));
+  const int64_t workgroups = (rows * row_vecs + 256 * kUnroll - 1) / (256 * kUnroll);
   auto go = [&](auto t, auto f) {
     typedef decltype(t) T;
-    quantize_mx_kernel<T, decltype(f)::value>
-        <<<grid, 256, 0, st>>>(static_cast<const T*>(x), x_row, rows, (int)k, row_vecs,
-                               static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales));
-    return hipGetLastError();
+    return in_parts(workgroups, 256, [&](int64_t from, dim3 grid) {
+      quantize_mx_kernel<T, decltype(f)::value>
+          <<<grid, 256, 0, st>>>(static_cast<const T*>(x), x_row, rows, (int)k, row_vecs,
+                                 static_cast<uint8_t*>(codes), static_cast<uint8_t*>(scales), from);
+    });
   };
   auto by_type = [&](auto f) {
     switch (dtype) {
