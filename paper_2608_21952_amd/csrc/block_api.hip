@@ -22,6 +22,73 @@ bool bad_size(int64_t v, int64_t least) { return v < least || v >= kMaxSize; }
 bool bad_stride(int64_t v) { return v < 0 || v > kMaxStride; }
 ssdi8_status status_of(hipError_t e) { return e == hipSuccess ? SSDI8_OK : SSDI8_ERR_HIP; }
 
+// A launch has fewer than 2^32 threads.  Calls of more run in parts: f(first, count) for batch elements or rows of which
+// each has `threads` at most.  Parts begin at multiples of 64, so that what lies behind one another stays aligned.
+template <typename F> hipError_t parts(int64_t items, double threads, F f) {
+  const double fit = 2147483648.0 / threads;
+  const int64_t most = fit > 1.0e12 ? items : fit < 64.0 ? 64 : (int64_t)fit / 64 * 64;
+  hipError_t e = hipSuccess;
+  for (int64_t first = 0; first < items && e == hipSuccess; first += most)
+    e = f(first, items - first < most ? items - first : most);
+  return e;
+}
+const void* ahead(const void* p, int64_t bytes) { return p ? static_cast<const char*>(p) + bytes : nullptr; }
+void* ahead(void* p, int64_t bytes) { return p ? static_cast<char*>(p) + bytes : nullptr; }
+
+ssdi8::ConvOut outputs_of(const ssdi8::ConvOut& out, int64_t rows, uintptr_t es) {
+  ssdi8::ConvOut o = out;
+  for (int i = 0; i < 3; ++i) o.y[i] = ahead(out.y[i], rows * (out.end[i] - (i ? out.end[i - 1] : 0)) * (int64_t)es);
+  return o;
+}
+
+// Batch elements from b on, n of them.
+ssdi8::SelScan scan_of(const ssdi8::SelScan& a, int64_t b, int64_t n) {
+  const int64_t es = (int64_t)size_of(a.dtype), D = a.nheads * a.headdim;
+  ssdi8::SelScan s = a;
+  s.batch = n;
+  s.u = ahead(a.u, b * a.ur.batch * es);
+  s.dt = ahead(a.dt, b * a.dtr.batch * (int64_t)size_of(a.dt_dtype));
+  s.B = ahead(a.B, b * a.Br.batch * es);
+  s.C = ahead(a.C, b * a.Cr.batch * es);
+  s.z = ahead(a.z, b * a.zr.batch * es);
+  if (a.init) s.init = a.init + b * D * a.dstate;
+  if (a.lengths) s.lengths = a.lengths + b;
+  s.y = ahead(a.y, b * a.seqlen * D * es);
+  if (a.final_state) s.final_state = a.final_state + b * D * a.dstate;
+  return s;
+}
+// Threads of a batch element at most: workgroups of 256 for four channels of a group.
+double scan_threads(const ssdi8_sel_scan_dims* d) {
+  return ((double)d->nheads * (double)d->headdim / 4.0 + (double)d->ngroups) * 256.0;
+}
+
+hipError_t linear(const ssdi8::LinearArgs& a, hipStream_t st) {
+  // 256 threads for 64 x 64 values, of few rows 512 for 16 outputs; more for each only where they are few in all
+  const double threads = a.m > 64 ? ((double)a.m / 64.0 + 1.0) * ((double)a.n / 64.0 + 1.0) * 256.0
+                                  : ((double)a.n / 16.0 + 1.0) * 512.0;
+  if (threads < 4294967296.0) return ssdi8::launch_linear(a, st);
+  const int64_t es = (int64_t)size_of(a.dtype), ys = (int64_t)size_of(a.out_dtype);
+  ssdi8::LinearArgs lo = a, hi = a;
+  if (a.m > 64 && a.m >= a.n) {
+    lo.m = a.m / 128 * 64;
+    hi.m = a.m - lo.m;
+    hi.x = ahead(a.x, lo.m * a.x_row * es);
+    if (a.x_scale) hi.x_scale = a.x_scale + lo.m;
+    hi.residual = ahead(a.residual, lo.m * a.residual_row * ys);
+    hi.y = ahead(a.y, lo.m * a.y_row * ys);
+  } else {
+    lo.n = a.n / 128 * 64;
+    hi.n = a.n - lo.n;
+    hi.w = ahead(a.w, lo.n * a.w_row * es);
+    if (a.w_scale) hi.w_scale = a.w_scale + lo.n;
+    if (a.bias) hi.bias = a.bias + lo.n;
+    hi.residual = ahead(a.residual, lo.n * ys);
+    hi.y = ahead(a.y, lo.n * ys);
+  }
+  const hipError_t e = linear(lo, st);
+  return e == hipSuccess ? linear(hi, st) : e;
+}
+
 ssdi8_status check_conv(int64_t batch, int64_t seqlen, int64_t channels, const ssdi8_conv_args* a,
                         bool step, ssdi8::ConvOut* out) {
   if (bad_size(batch, 0) || bad_size(seqlen, 0) || bad_size(channels, 1)) return SSDI8_ERR_SHAPE;
@@ -133,10 +200,16 @@ ssdi8_status ssdi8_causal_conv(int64_t batch, int64_t seqlen, int64_t channels,
   ssdi8::ConvOut out;
   const ssdi8_status s = check_conv(batch, seqlen, channels, a, false, &out);
   if (s != SSDI8_OK || batch == 0 || (seqlen == 0 && !a->final_state)) return s;
-  return status_of(ssdi8::launch_conv(
-      a->dtype, a->width, batch, seqlen, channels, a->x, {a->x_batch_stride, a->x_token_stride},
-      a->weight, a->bias, a->act == SSDI8_ACT_SILU, a->init_state, a->lengths, out, a->final_state,
-      (hipStream_t)stream));
+  const int64_t es = (int64_t)size_of(a->dtype), state = (int64_t)(a->width - 1) * channels * es;
+  // workgroups of 256 for 512 channels of 256 tokens (of fewer only where that leaves few of them)
+  const double threads = ((double)seqlen / 256.0 + 1.0) * ((double)channels / 512.0 + 4.0) * 256.0;
+  return status_of(parts(batch, threads, [&](int64_t b, int64_t n) {
+    return ssdi8::launch_conv(a->dtype, a->width, n, seqlen, channels, ahead(a->x, b * a->x_batch_stride * es),
+                              {a->x_batch_stride, a->x_token_stride}, a->weight, a->bias, a->act == SSDI8_ACT_SILU,
+                              ahead(a->init_state, b * state), a->lengths ? a->lengths + b : nullptr,
+                              outputs_of(out, b * seqlen, es), ahead(a->final_state, b * state),
+                              (hipStream_t)stream);
+  }));
 }
 
 ssdi8_status ssdi8_causal_conv_step(int64_t batch, int64_t channels, const ssdi8_conv_args* a,
@@ -144,10 +217,12 @@ ssdi8_status ssdi8_causal_conv_step(int64_t batch, int64_t channels, const ssdi8
   ssdi8::ConvOut out;
   const ssdi8_status s = check_conv(batch, 1, channels, a, true, &out);
   if (s != SSDI8_OK || batch == 0) return s;
-  return status_of(ssdi8::launch_conv_step(a->dtype, a->width, batch, channels, a->x,
-                                           a->x_batch_stride, a->weight, a->bias,
-                                           a->act == SSDI8_ACT_SILU, a->final_state, out,
-                                           (hipStream_t)stream));
+  const int64_t es = (int64_t)size_of(a->dtype), state = (int64_t)(a->width - 1) * channels * es;
+  return status_of(parts(batch, ((double)channels / 512.0 + 4.0) * 64.0, [&](int64_t b, int64_t n) {
+    return ssdi8::launch_conv_step(a->dtype, a->width, n, channels, ahead(a->x, b * a->x_batch_stride * es),
+                                   a->x_batch_stride, a->weight, a->bias, a->act == SSDI8_ACT_SILU,
+                                   ahead(a->final_state, b * state), outputs_of(out, b, es), (hipStream_t)stream);
+  }));
 }
 
 size_t ssdi8_selective_scan_workspace_size(const ssdi8_sel_scan_dims* d) {
@@ -164,7 +239,11 @@ ssdi8_status ssdi8_selective_scan(const ssdi8_sel_scan_dims* d, const ssdi8_sel_
   if (s != SSDI8_OK || d->batch == 0 || (d->seqlen == 0 && !a->final_state)) return s;
   const size_t need = ssdi8_selective_scan_workspace_size(d);
   if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return SSDI8_ERR_WORKSPACE;
-  return status_of(ssdi8::launch_sel_scan(scan, (hipStream_t)stream));
+  return status_of(parts(d->batch, scan_threads(d), [&](int64_t b, int64_t n) {
+    ssdi8::SelScan s = scan_of(scan, b, n);
+    if (n < d->batch) s.workspace = nullptr;   // uncut, as the whole is: a short last part would be cut into spans
+    return ssdi8::launch_sel_scan(s, (hipStream_t)stream);
+  }));
 }
 
 ssdi8_status ssdi8_selective_scan_step(const ssdi8_sel_scan_dims* d, const ssdi8_sel_scan_args* a,
@@ -173,7 +252,10 @@ ssdi8_status ssdi8_selective_scan_step(const ssdi8_sel_scan_dims* d, const ssdi8
   ssdi8_status s = check_scan_dims(d, true);
   if (s == SSDI8_OK) s = check_scan(d, a, true, &scan);
   if (s != SSDI8_OK || d->batch == 0) return s;
-  return status_of(ssdi8::launch_sel_scan_step(scan, a->final_state, (hipStream_t)stream));
+  return status_of(parts(d->batch, scan_threads(d), [&](int64_t b, int64_t n) {
+    const ssdi8::SelScan s = scan_of(scan, b, n);
+    return ssdi8::launch_sel_scan_step(s, s.final_state, (hipStream_t)stream);
+  }));
 }
 
 ssdi8_status ssdi8_gated_norm(int64_t rows, int64_t channels, int64_t groups,
@@ -182,6 +264,9 @@ ssdi8_status ssdi8_gated_norm(int64_t rows, int64_t channels, int64_t groups,
     return SSDI8_ERR_SHAPE;
   if ((double)rows * channels > kMaxCount || (double)rows * groups > kMaxGrid) return SSDI8_ERR_SHAPE;
   if (channels / groups > 32768) return SSDI8_ERR_UNSUPPORTED;
+  const int64_t width = channels / groups;
+  const double threads = (double)groups * (width > 8192 ? 1024.0 : width > 1024 ? 512.0 : 64.0);
+  if (threads * 64.0 >= 4294967296.0) return SSDI8_ERR_UNSUPPORTED;   // of a row: 64 rows are in one launch
   if (!a) return SSDI8_ERR_NULL;
   if (!is_float(a->dtype)) return SSDI8_ERR_ARG;
   if (!(a->eps >= 0.0f) || a->eps > 3.0e38f) return SSDI8_ERR_ARG;
@@ -193,10 +278,13 @@ ssdi8_status ssdi8_gated_norm(int64_t rows, int64_t channels, int64_t groups,
   if (off(a->x, es) || off(a->z, es) || off(a->residual, es) || off(a->residual_out, es) ||
       off(a->y, es) || off(a->weight, 4))
     return SSDI8_ERR_ALIGN;
-  return status_of(ssdi8::launch_gated_norm(a->dtype, rows, channels, groups, a->x, a->x_row_stride,
-                                            a->z, a->z_row_stride, a->residual, a->weight, a->eps,
-                                            a->norm_before_gate != 0, a->y, a->residual_out,
-                                            (hipStream_t)stream));
+  return status_of(parts(rows, threads, [&](int64_t r, int64_t n) {
+    const int64_t in = r * channels * (int64_t)es;
+    return ssdi8::launch_gated_norm(a->dtype, n, channels, groups, ahead(a->x, r * a->x_row_stride * (int64_t)es),
+                                    a->x_row_stride, ahead(a->z, r * a->z_row_stride * (int64_t)es), a->z_row_stride,
+                                    ahead(a->residual, in), a->weight, a->eps, a->norm_before_gate != 0, ahead(a->y, in),
+                                    ahead(a->residual_out, in), (hipStream_t)stream);
+  }));
 }
 
 ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_linear_args* a,
@@ -245,7 +333,7 @@ ssdi8_status ssdi8_linear(int64_t rows, int64_t outputs, int64_t k, const ssdi8_
   l.residual_row = a->residual_row_stride;
   l.y = a->y;
   l.y_row = a->y_row_stride;
-  return status_of(ssdi8::launch_linear(l, (hipStream_t)stream));
+  return status_of(linear(l, (hipStream_t)stream));
 }
 
 }  // extern "C"

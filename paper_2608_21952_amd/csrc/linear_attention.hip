@@ -873,12 +873,12 @@ __device__ __forceinline__ void store4(float* p, float4 f) {
 // threads.  Bound by the state's bytes: all of a thread's loads are on their way before the first is used.  128 x 80 heads
 // of 128 x 64: 119 us, 5.7 TB/s (154 through the caches).
 template <typename T, int kRows>
-__global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, int slices, int64_t first) {
+__global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, int slices, unsigned first) {
   constexpr int kMost = kRows * 16;
   __shared__ float k_lds[kMost], q_lds[kMost];
   __shared__ float sums[4][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t id = first + blockIdx.x;
+  const unsigned id = first + blockIdx.x;
   const int slice = (int)(id % slices);
   const int64_t head = id / slices, b = head / a.v_heads;
   const int hv = (int)(head % a.v_heads), keys = (int)a.keys;
@@ -1053,9 +1053,9 @@ template <typename T> hipError_t by_size(const Args& p, hipStream_t st) {
 template <typename T> hipError_t run_step(const LinearAttention& a, hipStream_t st) {
   const int slices = (int)((a.values + 63) / 64);
   return in_parts(a.batch * a.v_heads * slices, 256, [&](int64_t first, dim3 grid) {
-    if (a.keys <= 64) attention_step_kernel<T, 4><<<grid, 256, 0, st>>>(a, slices, first);
-    else if (a.keys <= 128) attention_step_kernel<T, 8><<<grid, 256, 0, st>>>(a, slices, first);
-    else attention_step_kernel<T, 16><<<grid, 256, 0, st>>>(a, slices, first);
+    if (a.keys <= 64) attention_step_kernel<T, 4><<<grid, 256, 0, st>>>(a, slices, (unsigned)first);
+    else if (a.keys <= 128) attention_step_kernel<T, 8><<<grid, 256, 0, st>>>(a, slices, (unsigned)first);
+    else attention_step_kernel<T, 16><<<grid, 256, 0, st>>>(a, slices, (unsigned)first);
   });
 }
 

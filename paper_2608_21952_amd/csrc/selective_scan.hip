@@ -180,7 +180,7 @@ hipError_t launch_sel_scan(const SelScan& a, hipStream_t st) {
   p.s = a;
   p.D = (int)(a.nheads * a.headdim);
   p.group_ch = p.D / (int)a.ngroups;
-  p.spans = sel_scan_spans(a.batch, a.seqlen, p.D, a.ngroups, a.dstate);
+  p.spans = a.workspace ? sel_scan_spans(a.batch, a.seqlen, p.D, a.ngroups, a.dstate) : 1;
   const int64_t tokens = (a.seqlen + p.spans - 1) / p.spans;
   p.span = (tokens + kSpanTokens - 1) / kSpanTokens * kSpanTokens;
   // rounding up may leave spans without tokens: fewer are launched
