@@ -345,9 +345,15 @@ hipError_t quantize_impl(const T* src, int64_t b, int64_t l, int64_t k, int64_t 
                          (uint32_t)rows);
       return hipGetLastError();
     }
-    hipLaunchKernelGGL(quant_token_dynamic<T>, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0,
-                       st, src, dst, scale, rows, m);
-    return hipGetLastError();
+    // a launch has fewer than 2^32 threads
+    for (int64_t r = 0; r < rows; r += (int64_t)1 << 25) {
+      const int64_t some = rows - r < ((int64_t)1 << 25) ? rows - r : (int64_t)1 << 25;
+      hipLaunchKernelGGL(quant_token_dynamic<T>, dim3((unsigned)((some + 3) / 4)), dim3(256), 0, st, src + r * m,
+                         dst + r * m, scale + r, some, m);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   }
   if (compute_scale) {
     const int ngran = gran == 0 ? 1 : (gran == 1 ? (int)k : (int)(k * m));

@@ -121,3 +121,12 @@ def test_linear(ssdi8, m, n, k):
     for s in parts(n) if n > m else parts(m):
         got = ssdi8.linear(x, w[s].clone(), bias=bias[s].clone()) if n > m else ssdi8.linear(x[s].clone(), w, bias=bias)
         assert torch.equal(got, y[:, s] if n > m else y[s])
+
+
+def test_quantize_act(ssdi8):
+    n = 2 ** 26 + 5
+    x = normal(1, n, 1, 8)
+    codes, steps = ssdi8.quantize_act(x, "token")
+    for s in parts(n):
+        part = ssdi8.quantize_act(x[:, s].clone(), "token")
+        assert torch.equal(part[0], codes[:, s]) and torch.equal(part[1], steps[s])
