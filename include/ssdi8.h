@@ -540,7 +540,8 @@ ssdi8_status ssdi8_linear_attention_step(const ssdi8_attn_dims* d, const ssdi8_a
 /*
  * Values in few bits, row by row:
  *   SSDI8_FMT_I8     int8 codes [rows, k] and an fp32 step per row, max|row| / 127 (1 for a row of zeros; at least the
- *                    smallest normal number): code = rne(value / step); what ssdi8_linear takes as int8 x.
+ *                    smallest normal number): code = rne(fl32(value * fl32(1 / step))), as ssdi8_quantize_act's; what
+ *                    ssdi8_linear takes as int8 x.
  *   SSDI8_FMT_MXFP8  blocks of 32 values, k filled up with zeros to whole blocks: e4m3 codes, a byte each
  *                    [rows, 32 blocks], and a scale byte per block [rows, blocks], 2^(byte - 127).
  *   SSDI8_FMT_MXFP4  the same with e2m1 codes, two to a byte, the even value in the low half [rows, 16 blocks].

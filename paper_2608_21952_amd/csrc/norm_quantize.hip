@@ -1,6 +1,6 @@
 // RMS norm of rows with an optional residual in front, an optional gate and groups of channels (the formulas of
 // norm.hip), its output in few bits:
-//   int8           step = max |y| / 127 of the row (1 where all are 0), code = rne(y / step)
+//   int8           step = max |y| / 127 of the row (1 where all are 0), code = rne(y (1 / step))
 //   e4m3, e2m1     blocks of 32 channels with a power of two each (mx.hpp)
 // The codes are those of the unrounded y; y itself, rounded, is written too where it is wanted.  A row (int8) or a
 // block with an infinity or a NaN has a scale of NaN and codes of 0.
