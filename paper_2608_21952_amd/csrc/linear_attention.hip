@@ -13,21 +13,22 @@
 // out so that they are keys 8 g + (0..7), the ones that a read of 16 bytes of q gives.
 //
 // Roundings, of 16-bit types: p and S are rounded once on their way into the products for y, which adds to y's error
-// about as much as its own rounding (0.00029 against 0.00021 of y, fp16): as two values each the same walk took 343 us
-// instead of 220.  exp(c_C - c_j) v_j, which would leave its rounding in S with every chunk, enters as the sum of three
-// bf16 values (two would be 2^-17 off), for fp16 too: two fp16 values, brought into range by a power of two per column,
-// lost what decays within a chunk had made small, though a key that is 0 for the later tokens has nothing else.  k of
-// fp16 enters as two bf16 values then: five products where two fp16 values take two, 314 us instead of 246 for 4 x 4096
-// tokens of 80 heads.  fp16: p per row and S per column are brought to the type's range by powers of two.
+// about as much as its own rounding (0.00029 against 0.00021 of y, fp16): as two values each a call takes 316 us
+// instead of 292 (4 x 4096 tokens of 80 heads, fp16), 221 instead of 207 (4 x 8192 of 16 heads, bf16).  fp16: p per row
+// and S per column are brought to the top of the type's range by powers of two.  exp(c_C - c_j) v_j, which would leave its
+// rounding in S with every chunk, enters as the sum of three bf16 values (two would be 2^-17 off), of fp16 too: two fp16
+// values, brought into range by a power of two per column, lose what decays within a chunk have made small, though a key
+// that is 0 for the later tokens has nothing else.  k of fp16 enters as two bf16 values then, five products in all: 4 x
+// 4096 tokens of 80 heads 292 us, 232 in bf16, whose k is one value.
 // Sums, S, and the decays' sums (these in fp64: differences of far sums) are not rounded.
 // A value of v that is no number would reach earlier tokens of its chunk through 0 times it: it enters as 0, and its
 // column is NaN from its token on.
 //
-// What bounds it: of a chunk's 9 us with two workgroups on a CU the products take 2; the rest is LDS reads of the
+// What bounds it: of a chunk's 9 us with two workgroups on a CU (fp16) the products take 3; the rest is LDS reads of the
 // operands, S's conversion for every chunk, and the barriers between the phases.  Two heads that share q and k read them once.
-// 4 x 4096 tokens, 80 heads of 64 with shared q and k of 128, fp16: 179 us, with the spans' states 80 and their join 13
-// beside them (1.5 TB/s in all); 4 x 8192, 16 heads of 128 x 128, bf16: 156 + 83 + 13; 16384 of 8 heads of 64 x 128, fp32:
-// 77 + 39 + 10.
+// 4 x 4096 tokens, 80 heads of 64 with shared q and k of 128, fp16: 185 us, with the spans' states 94 and their join 12
+// beside them (1.2 TB/s in all); 4 x 8192, 16 heads of 128 x 128, bf16: 123 + 69 + 14; 16384 of 8 heads of 64 x 128, fp32:
+// 71 + 36 + 10.
 #include <type_traits>
 #include <utility>
 
@@ -877,7 +878,8 @@ __device__ __forceinline__ void store4(float* p, float4 f) {
 
 // One token.  A workgroup takes 64 columns of a head's state: 16 threads of four columns each, 16 such rows of
 // threads.  Bound by the state's bytes: all of a thread's loads are on their way before the first is used.  128 x 80 heads
-// of 128 x 64: 119 us, 5.7 TB/s (154 through the caches).
+// of 128 x 64: 119 us, 5.7 TB/s, 134 through the caches, with other states in between.  The same states token after token,
+// past the caches / through them: 21 MB 8.5 / 8.7, 42 MB 12.9 / 15.4, 84 MB 27 / 28, 168 MB 58 / 53, 336 MB 120 / 117.
 template <typename T, int kRows>
 __global__ __launch_bounds__(256) void attention_step_kernel(LinearAttention a, int slices, unsigned first) {
   constexpr int kMost = kRows * 16;
@@ -983,8 +985,8 @@ bool paired(const LinearAttention& a) {
 }
 
 // Columns of a workgroup: 64 where 128 would leave half of the card without work, even with the tokens cut into spans of
-// four chunks: a narrow workgroup is through a chunk sooner.  us with 64 / 128: 1 x 256 tokens, 16 heads of 128 x 128 19 / 26,
-// 4 x 256, 64 heads 31 / 34, 4 x 2000, 8 heads 56 / 63; above, q k is formed twice: 4 x 8192, 16 heads 220 with 128.
+// four chunks: a narrow workgroup is through a chunk sooner.  us with 64 / 128, bf16: 1 x 256 tokens, 16 heads of 128 x 128
+// 19 / 26, 4 x 256, 64 heads 28 / 32, 4 x 2000, 8 heads 51 / 61; above, q k is formed twice: 4 x 8192, 16 heads 235 / 205.
 int64_t slice_of(const LinearAttention& a) {
   if (a.values <= 64 || a.keys > 128) return 64;
   const int64_t chunks = (a.seqlen + chunk_of(a.dtype) - 1) / chunk_of(a.dtype), spans = chunks < 8 ? 1 : chunks / 4;
@@ -1000,7 +1002,8 @@ Args plan(const LinearAttention& a) {
   p.chunks = (int)((a.seqlen + c - 1) / c);
   p.groups = (int)(paired(a) ? a.heads / 2 : a.heads);
   // Spans: as many workgroups as the card holds at once (two for every CU), each with two chunks at least; none of
-  // fewer than eight chunks.  us with and without: 8 chunks of 8 heads of 128 x 128 28 / 37, four chunks of 16 heads 27 / 19.
+  // fewer than eight chunks.  us with and without, bf16: 8 chunks of 8 heads of 128 x 128 29 / 32, four chunks of 16 heads
+  // 27 / 19.
   const int64_t wgs = a.batch * p.groups * p.slices, hold = a.keys > 128 ? 256 : 512, most = p.chunks < 8 ? 1 : p.chunks / 2;
   int64_t spans = wgs == 0 ? 1 : hold / wgs;
   spans = spans < most ? spans : most;

@@ -12,8 +12,8 @@
 // in registers.  LDS holds 16-byte chunk c of a line (128 bytes) of row r at slot c ^ (r / 2 % 8), so that the
 // 16 lanes that a fragment read serves at a time touch every bank once.
 // What bounds it: the way of the operands into LDS (a tile of 128 x 128 needs 32 KB for 512 cycles of a SIMD's products)
-// and the way out; 16384 x 10496 x 2560 395 us (2.2 PFLOP/s, the vendor's library 456; products from registers alone
-// reach 5.7), with e4m3 x 508 (library, both operands e4m3, 775).  Tiles of 256 x 256 did not fit the registers.
+// and the way out; 16384 x 10496 x 2560 382 us (2.3 PFLOP/s, the vendor's library 402; products from registers alone
+// reach 5.7), with e4m3 x 524 (library, both operands e4m3, 678).  Tiles of 256 x 256 did not fit the registers.
 // Few rows (mx_rows): bound by the bytes of w.  A workgroup takes 16 rows of w, its waves share k by lines of 128
 // bytes, each straight from memory into the matrix instruction's registers, and their sums meet in LDS.
 #include "common.hpp"
@@ -402,21 +402,25 @@ template <int kX, int kBM, int kBN, int kWM, int kWN> hipError_t run_tile(const 
 
 template <int kX> hipError_t by_tiles(const LinearMx& a, hipStream_t st) {
   auto count = [&](int64_t bm, int64_t bn) { return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn); };
-  // Small tiles where large ones leave CUs without work: us with 64 x 64 / 128 x 128 e2m1 512 x 5120 x 2560 12.6 / 12.8,
-  // 1000 x 2900 x 992 10.3 / 10.7, 2048 x 2560 x 5120 42.3 / 38.4; e4m3 with 128 x 256 15.2 / 22.0, 11.1 / 16.3, 49.6 / 42.9.
+  // Small tiles where large ones leave CUs without work: us with 64 x 64 / 128 x 128 e2m1 512 x 5120 x 2560 12.4 / 12.6,
+  // 1000 x 2900 x 992 11.1 / 11.9, 2048 x 2560 x 5120 43.5 / 39.4; e4m3 with 128 x 256 15.0 / 22.6, 12.1 / 17.6, 50.3 / 43.8.
   if constexpr (kX == kE4m3) {
     if (count(128, 256) < 128) return run_tile<kX, 64, 64, 2, 2>(a, st);
     return run_tile<kX, 128, 256, 2, 4>(a, st);
   } else {
     if (count(128, 128) < 256) return run_tile<kX, 64, 64, 2, 2>(a, st);
-    // Eight waves where a tile's way out is much of its time, four (more products per value read from LDS) over a long k:
-    // 16384 x 10496 x 2560 395 / 469, 16384 x 768 x 1536 24 / 28, 16384 x 2560 x 5120 210 / 179, 2048 x 2560 x 5120 45 / 38.
+    // Eight waves where a tile's way out is much of its time, four (more products per value read from LDS) over a long k.
+    // us with eight / four: 16384 x 768 of k 1024 22 / 25, 2560 32 / 36, 3584 42 / 44, 4096 54 / 48, 5120 68 / 56; 16384 x 2560
+    // of 1024 55 / 60, 2560 95 / 98, 3584 130 / 123, 4096 165 / 141, 8192 318 / 261; 4096 x 4096 of 3584 54 / 55, 4096 71 / 62;
+    // 16384 x 10496 x 2560 382 / 372.
     if (a.blocks >= 128) return run_tile<kX, 128, 128, 2, 2>(a, st);
     return run_tile<kX, 128, 128, 2, 4>(a, st);
   }
 }
 
 template <int kX> hipError_t run(const LinearMx& a, hipStream_t st) {
+  // us up to 32 rows, with mx_rows / 64 x 64 tiles, e4m3 x: 16 x 10496 x 2560 8.0 / 7.6, 16 x 2560 x 5120 6.7 / 11.7, 32 x
+  // 1024 x 8192 13.6 / 17.1, 32 x 768 x 1536 4.3 / 6.3; against it, many outputs: 32 x 10496 x 2560 12.0 / 8.1.
   if (a.m > 32) return by_tiles<kX>(a, st);
   return in_parts((a.n + 15) / 16, 512, [&](int64_t first, dim3 grid) {
     if (a.m <= 16) mx_rows<kX, 1, 8><<<grid, 512, 0, st>>>(a, first);

@@ -10,9 +10,10 @@
 // threads walk rows with their weights in registers and the next row's values on their way.  A thread holds vectors
 // of eight channels, so that a block of 32 is that of four neighbouring lanes.  With several groups the sums of
 // vectors meet in LDS and a wave adds up each group's, in one order.  Rows of more than 8192 channels, and groups whose
-// width is no multiple of eight, have their values in LDS instead of registers.
-// 16384 x 5120 fp16 with gate to e4m3 97 us (4.3 TB/s), 16384 x 2560 bf16 with residual and its sum 57 (5.2 TB/s); with
-// several vectors of a wide row in a thread the first took 11 us more.
+// width is no multiple of eight, have their values in LDS instead of registers, a row at a time.
+// 16384 x 5120 fp16 with gate to e4m3 97 us (4.3 TB/s), to int8 118, as the workgroup meets once more for a row; 16384 x 2560
+// bf16 with residual and its sum 57 (5.2 TB/s), 58.  In LDS: 16384 x 5121 fp16 with gate 177, int8 235 (2.4 and 1.8 TB/s),
+// 8192 x 10240 144, 187.
 #include "mx.hpp"
 
 namespace ssdi8 {
@@ -360,8 +361,8 @@ template <typename T> hipError_t run(const Args& a, hipStream_t st) {
   auto launch = [&](auto wave, auto most, auto limit, auto groups, int threads) {
     constexpr bool kWave = decltype(wave)::value, kGroups = decltype(groups)::value;
     constexpr int kItems = kWave ? 4 : 1;
-    // rows of a walk: as many as leave every CU eight workgroups, four at most (16384 x 5120 with gate: 109 us at two,
-    // 104 at four and eight; 16384 x 2560 with residual 53, 49, 54)
+    // rows of a walk: as many as leave every CU eight workgroups, four at most (us at one, two, four, eight: 16384 x 5120
+    // with gate 113, 101, 97, 98; 16384 x 2560 with residual 60, 54, 57, 63)
     int walk = 1;
     while (walk < 4 && a.rows / (2 * walk) >= 2048 * kItems) walk *= 2;
     const int64_t count = (a.rows + walk - 1) / walk;
@@ -382,7 +383,7 @@ template <typename T> hipError_t run(const Args& a, hipStream_t st) {
     using W = integral_constant<int, 256>;
     if (vecs <= 64) return launch(std::true_type(), One(), W(), groups, 256);
     if (vecs <= 128) return launch(std::true_type(), Two(), W(), groups, 256);
-    // A vector per thread: two of them left half as many waves (16384 x 5120 with gate 118 us, 104 with one).
+    // A vector per thread: two of them left half as many waves (16384 x 5120 with gate 111 us, 97 with one).
     return launch(std::false_type(), One(), integral_constant<int, 1024>(), groups, (vecs + 63) / 64 * 64);
   };
   return a.groups == 1 ? by_width(std::false_type()) : by_width(std::true_type());
