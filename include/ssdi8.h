@@ -350,6 +350,9 @@ ssdi8_status ssdi8_calibrate(const ssdi8_dims* d, const ssdi8_calib_args* a, voi
  *     (taken into [0, seqlen]) are not read, give y = 0 and leave the state as it is.
  *   - An output may not overlap an input, except where a call says so.
  *   - batch = 0 or no rows: nothing is done.  seqlen = 0: the final state is the initial one.
+ *   - Batch elements, rows and outputs are not limited by what one launch holds (2^32 threads): more run in several.
+ *     One batch element or row that is more by itself is refused (SSDI8_ERR_UNSUPPORTED): a norm of 2^26 groups, a
+ *     scan of 2^26 channels of 256 states.
  */
 
 /*

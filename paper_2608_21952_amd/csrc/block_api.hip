@@ -23,10 +23,10 @@ bool bad_stride(int64_t v) { return v < 0 || v > kMaxStride; }
 ssdi8_status status_of(hipError_t e) { return e == hipSuccess ? SSDI8_OK : SSDI8_ERR_HIP; }
 
 // A launch has fewer than 2^32 threads.  Calls of more run in parts: f(first, count) for batch elements or rows of which
-// each has `threads` at most.  Parts begin at multiples of 64, so that what lies behind one another stays aligned.
+// each has `threads` at most, fewer than kMaxThreads.
+constexpr double kMaxThreads = 4294967296.0;
 template <typename F> hipError_t parts(int64_t items, double threads, F f) {
-  const double fit = 2147483648.0 / threads;
-  const int64_t most = fit > 1.0e12 ? items : fit < 64.0 ? 64 : (int64_t)fit / 64 * 64;
+  const int64_t most = threads < kMaxThreads / 2.0 ? (int64_t)(kMaxThreads / 2.0 / threads) : 1;
   hipError_t e = hipSuccess;
   for (int64_t first = 0; first < items && e == hipSuccess; first += most)
     e = f(first, items - first < most ? items - first : most);
@@ -57,16 +57,17 @@ ssdi8::SelScan scan_of(const ssdi8::SelScan& a, int64_t b, int64_t n) {
   if (a.final_state) s.final_state = a.final_state + b * D * a.dstate;
   return s;
 }
-// Threads of a batch element at most: workgroups of 256 for four channels of a group.
+// Threads of a batch element at most: 8 to 64 for a channel by its states, and a workgroup's end for each group.
 double scan_threads(const ssdi8_sel_scan_dims* d) {
-  return ((double)d->nheads * (double)d->headdim / 4.0 + (double)d->ngroups) * 256.0;
+  const double lanes = d->dstate <= 32 ? 8.0 : d->dstate <= 64 ? 16.0 : d->dstate <= 128 ? 32.0 : 64.0;
+  return (double)d->nheads * (double)d->headdim * lanes + (double)d->ngroups * 256.0;
 }
 
 hipError_t linear(const ssdi8::LinearArgs& a, hipStream_t st) {
   // 256 threads for 64 x 64 values, of few rows 512 for 16 outputs; more for each only where they are few in all
   const double threads = a.m > 64 ? ((double)a.m / 64.0 + 1.0) * ((double)a.n / 64.0 + 1.0) * 256.0
                                   : ((double)a.n / 16.0 + 1.0) * 512.0;
-  if (threads < 4294967296.0) return ssdi8::launch_linear(a, st);
+  if (threads < kMaxThreads) return ssdi8::launch_linear(a, st);
   const int64_t es = (int64_t)size_of(a.dtype), ys = (int64_t)size_of(a.out_dtype);
   ssdi8::LinearArgs lo = a, hi = a;
   if (a.m > 64 && a.m >= a.n) {
@@ -131,6 +132,7 @@ ssdi8_status check_scan_dims(const ssdi8_sel_scan_dims* d, bool step) {
   if (D >= (double)kMaxSize - 4096) return SSDI8_ERR_SHAPE;
   if (d->nheads * d->headdim % d->ngroups != 0) return SSDI8_ERR_SHAPE;
   if (d->dstate > 256) return SSDI8_ERR_UNSUPPORTED;
+  if (scan_threads(d) >= kMaxThreads) return SSDI8_ERR_UNSUPPORTED;
   if ((double)d->batch * L * D > kMaxCount || (double)d->batch * D * 256 * 64 > kMaxCount * 16 ||
       (double)d->batch * L * d->ngroups * d->dstate > kMaxCount ||
       (double)d->batch * (D / 2 + d->ngroups) > kMaxGrid || L * 0.5 > kMaxGrid)
@@ -203,6 +205,7 @@ ssdi8_status ssdi8_causal_conv(int64_t batch, int64_t seqlen, int64_t channels,
   const int64_t es = (int64_t)size_of(a->dtype), state = (int64_t)(a->width - 1) * channels * es;
   // workgroups of 256 for 512 channels of 256 tokens (of fewer only where that leaves few of them)
   const double threads = ((double)seqlen / 256.0 + 1.0) * ((double)channels / 512.0 + 4.0) * 256.0;
+  if (threads >= kMaxThreads) return SSDI8_ERR_UNSUPPORTED;
   return status_of(parts(batch, threads, [&](int64_t b, int64_t n) {
     return ssdi8::launch_conv(a->dtype, a->width, n, seqlen, channels, ahead(a->x, b * a->x_batch_stride * es),
                               {a->x_batch_stride, a->x_token_stride}, a->weight, a->bias, a->act == SSDI8_ACT_SILU,
@@ -266,7 +269,7 @@ ssdi8_status ssdi8_gated_norm(int64_t rows, int64_t channels, int64_t groups,
   if (channels / groups > 32768) return SSDI8_ERR_UNSUPPORTED;
   const int64_t width = channels / groups;
   const double threads = (double)groups * (width > 8192 ? 1024.0 : width > 1024 ? 512.0 : 64.0);
-  if (threads * 64.0 >= 4294967296.0) return SSDI8_ERR_UNSUPPORTED;   // of a row: 64 rows are in one launch
+  if (threads >= kMaxThreads) return SSDI8_ERR_UNSUPPORTED;
   if (!a) return SSDI8_ERR_NULL;
   if (!is_float(a->dtype)) return SSDI8_ERR_ARG;
   if (!(a->eps >= 0.0f) || a->eps > 3.0e38f) return SSDI8_ERR_ARG;

@@ -106,6 +106,19 @@ def test_selective_scan_step(ssdi8):
         assert torch.equal(got, y[s]) and torch.equal(state[s], st)
 
 
+def test_selective_scan_step_of_many_channels(ssdi8):
+    """A batch element of 2^26 threads: fewer than 64 of them are a launch's."""
+    n, D, N = 67, 2 ** 20, 129
+    u, z, dt, B, C = normal(n, D), normal(n, D), normal(n, 1), normal(n, 1, N), normal(n, 1, N)
+    A, state = torch.full((1,), -1.0, device="cuda"), torch.empty(n, D, N, device="cuda").uniform_()
+    some = slice(n - 3, n)
+    want = state[some].clone()
+    y = ssdi8.selective_scan_step(u, dt, A, B, C, state, z=z)
+    assert torch.equal(ssdi8.selective_scan_step(*(t[some].clone() for t in (u, dt)), A, *(t[some].clone() for t in (B, C)), want,
+                                                 z=z[some].clone()), y[some])
+    assert torch.equal(state[some], want)
+
+
 def test_gated_norm(ssdi8):
     n, D = 2 ** 28 + 37, 8
     x, w = torch.empty(n, D, device="cuda", dtype=F16).normal_(), torch.full((D,), 2.0, device="cuda")
